@@ -492,12 +492,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
                           K + (((x >> 2) * L::kBlock + (x & 3) * 32) >> 4), kIdescS, part < L::kParts - 1 || x > 0);
             tc_commit(&s_full[s][buf]);
             if (half || k == steps - 1) release(slot_of(seq));
-            if (!kF32 && k == steps - 1) tc_commit(&q_free);
+            if (k == steps - 1) tc_commit(&q_free);
           }
           __syncwarp();
         }
       }
-      if (!kF32 && steps == 0 && leader) mbar_arrive(&q_free);
+      if (steps == 0 && leader) mbar_arrive(&q_free);
       n += steps;
       base += 2 * nt;
       ++piece;
@@ -624,7 +624,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_arrive(&q_full);
     };
     while (walk.next(q)) {
-      if (kF32) load_q(q);  // every S of the piece before is computed: its queries have been used
+      if (kF32) {
+        // Both product warps have passed the piece before: one without steps in it has no other tie to the streams, and
+        // would miss a phase of q_full
+        if (piece) wait(&q_free, (piece - 1) & 1);
+        load_q(q);
+      }
       const int nt = q.t1 - q.t0, steps = steps_of<L::kSingle>(q, s);
       const int row_item = (q.pair ? s * kTile : 0) + row, grow = q.row0 + row_item;  // row of the item; of the request and kv head
       const int node = min(grow >> p.g_shift, q.n - 1);

@@ -206,6 +206,17 @@ def test_32_bit_queries_keep_their_precision(kv, d):
     assert off ** 0.5 <= 2.0 ** -19 * whole ** 0.5, (off / whole) ** 0.5
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q,kv", [("f32", "f16"), ("f32", "bf16"), ("f16", "f16"), ("bf16", "bf16")])
+def test_pieces_of_one_tile_and_of_several_in_turn(q, kv, d):
+    """Runs of many pieces, of one tile (which one of a CTA's two streams takes alone) and of two to four, one behind the other."""
+    P = [(3, 250, 9, 100, 380, 60, 1, 130)[b % 8] for b in range(224)]
+    c = Case([1 + b % 3 for b in range(224)], P, 16, 8, d, q=q, kv=kv, seed=5)
+    for _ in range(5):
+        c.run()
+    c.check()
+
+
 def test_trees_that_begin_behind_other_nodes():
     """Nodes ahead of the first tree belong to nobody, whether items are cut between CTAs or not."""
     for lens in ([3000, 900], [5, 70]):
