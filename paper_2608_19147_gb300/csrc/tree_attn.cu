@@ -253,9 +253,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   // full, empty: a slot's tile has come, has been used by both streams; v_ready: a V tile (by its place among
   // the V tiles) is safe; q_full, q_free: the piece's queries are in place, have been used by both streams;
   // s_full, p_ready, o_done: a step's S is computed, its P written, P V added (in turn for a stream's steps);
-  // o_free: both streams have read the piece's O
+  // o_free: all have read a stream's O of a piece in which it has steps (a stream goes by its own pieces: one that
+  // counted the others' too would not follow the phases of those, and take an old one for the piece before)
   __shared__ uint64_t full[2 * L::kSlots], empty[L::kSlots], v_ready[L::kSlots], q_full, q_free, s_full[2][2], p_ready[2][2],
-      o_done[2][2], o_free;
+      o_done[2][2], o_free[2];
   __shared__ uint32_t s_tmem;
   // pieces (counted from 1) whose tree entries hold a V that is not finite; V tiles run at most kSlots pieces ahead
   __shared__ volatile int s_odd[2 * L::kSlots];
@@ -282,7 +283,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     if (tid == 0) {
       mbar_init(&q_full, kF32 ? kSoft : 1);
       mbar_init(&q_free, 2);
-      mbar_init(&o_free, 8);
+      mbar_init(&o_free[0], 8);
+      mbar_init(&o_free[1], 8);
     }
     mbar_fence_init();
   }
@@ -427,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const uint32_t S = tmem + s * kTile, O = tmem + 2 * kTile + s * kTile;
     const uint32_t ring = smem_addr(smem + L::kRing);
     Piece q;
-    uint32_t base = 0, piece = 0, n = 0;  // first ring place of the piece; the stream's steps before it
+    uint32_t base = 0, piece = 0, mine = 0, n = 0;  // first ring place of the piece; the stream's pieces and steps before it
     while (ok && walk.next(q)) {
       const int nt = __shfl_sync(0xffffffffu, q.t1 - q.t0, 0), steps = __shfl_sync(0xffffffffu, steps_of<L::kSingle>(q, s), 0);
       const bool pair = __shfl_sync(0xffffffffu, (int)q.pair, 0), every = pair || L::kSingle;
@@ -447,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           const uint32_t seq = base + v_seq(every, t, nt), nv = base / 2 + t, buf = (n + i) & 1, P = S + kStep * buf;
           const uint64_t V = smem_desc_sw128_mn(ring + slot_of(seq) * L::kSlot + half * (kStep * 128), L::kBlock);
           const int there = entries - (t0 + t) * kTile - half * kStep;  // entries from the step's first on
-          if (i == 0 && piece) wait(&o_free, (piece - 1) & 1);
+          if (i == 0 && mine) wait(&o_free[s], (mine - 1) & 1);
           if (!half) {
             wait(full_of(seq), full_turn(seq));
             wait(&v_ready[slot_of(nv)], turn_of(nv));
@@ -499,6 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       }
       if (steps == 0 && leader) mbar_arrive(&q_free);
       n += steps;
+      mine += steps > 0;
       base += 2 * nt;
       ++piece;
     }
@@ -790,8 +793,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         w1 = !both ? 0.f : y.x == M ? 1.f : exp2_fast(y.x - M);
         sum = both ? x.y * w0 + y.y * w1 : x.y;
       }
+      const int steps_1 = steps_of<L::kSingle>(q, 1);
       n_o[0] += steps_of<L::kSingle>(q, 0);
-      n_o[1] += steps_of<L::kSingle>(q, 1);
+      n_o[1] += steps_1;
       if (!q.pair || s == 0) wait_o(0, n_o[0] - 1);
       if (q.pair ? s == 1 : both) wait_o(1, n_o[1] - 1);
       __syncwarp();
@@ -884,7 +888,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&o_free);
+      if (lane == 0) {
+        mbar_arrive(&o_free[0]);  // the first stream has steps in every piece
+        if (steps_1 > 0) mbar_arrive(&o_free[1]);
+      }
       ++piece;
     }
   }

@@ -208,9 +208,10 @@ def test_32_bit_queries_keep_their_precision(kv, d):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("q,kv", [("f32", "f16"), ("f32", "bf16"), ("f16", "f16"), ("bf16", "bf16")])
-def test_pieces_of_one_tile_and_of_several_in_turn(q, kv, d):
+@pytest.mark.parametrize("lens", [(3, 250, 9, 100, 380, 60, 1, 130), (50, 140, 300), (100, 200)])
+def test_pieces_of_one_tile_and_of_several_in_turn(q, kv, d, lens):
     """Runs of many pieces, of one tile (which one of a CTA's two streams takes alone) and of two to four, one behind the other."""
-    P = [(3, 250, 9, 100, 380, 60, 1, 130)[b % 8] for b in range(224)]
+    P = [lens[b % len(lens)] for b in range(224)]
     c = Case([1 + b % 3 for b in range(224)], P, 16, 8, d, q=q, kv=kv, seed=5)
     for _ in range(5):
         c.run()
