@@ -254,9 +254,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   // the V tiles) is safe; q_full, q_free: the piece's queries are in place, have been used by both streams;
   // s_full, p_ready, o_done: a step's S is computed, its P written, P V added (in turn for a stream's steps);
   // o_free: all have read a stream's O of a piece in which it has steps (a stream goes by its own pieces: one that
-  // counted the others' too would not follow the phases of those, and take an old one for the piece before)
+  // counted the others' too would not follow the phases of those, and take an old one for the piece before); at_end:
+  // a stream's last product is done
   __shared__ uint64_t full[2 * L::kSlots], empty[L::kSlots], v_ready[L::kSlots], q_full, q_free, s_full[2][2], p_ready[2][2],
-      o_done[2][2], o_free[2];
+      o_done[2][2], o_free[2], at_end[2];
   __shared__ uint32_t s_tmem;
   // pieces (counted from 1) whose tree entries hold a V that is not finite; V tiles run at most kSlots pieces ahead
   __shared__ volatile int s_odd[2 * L::kSlots];
@@ -285,6 +286,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_init(&q_free, 2);
       mbar_init(&o_free[0], 8);
       mbar_init(&o_free[1], 8);
+      mbar_init(&at_end[0], 1);
+      mbar_init(&at_end[1], 1);
     }
     mbar_fence_init();
   }
@@ -381,6 +384,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         break;
       }
   };
+  // Whatever came before: what this role has under way is not left behind when the CTA ends.
+  auto drain = [](uint64_t* bar, uint32_t parity) {
+    for (uint32_t it = 0; it < (1u << 26) && !mbar_test_wait(bar, parity);) ++it;
+  };
   // the product of a stream's step; two steps back, it has been waited for before a step's S was begun
   auto wait_o = [&](int s, uint32_t step) { wait(&o_done[s][step & 1], (step >> 1) & 1); };
   // Order of a piece's tiles in the ring.  A stream for each half of the rows, or one only: K(0) V(0) K(1) V(1) ..;
@@ -419,6 +426,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
                         q.h, q.b, full_of(seq));
         }
       }
+      for (uint32_t i = seq > L::kSlots ? seq - L::kSlots : 0; i < seq; ++i) drain(full_of(i), full_turn(i));
     }
   } else if (warp < 3) {
     // ---- products, a warp per stream ----
@@ -505,14 +513,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       base += 2 * nt;
       ++piece;
     }
+    if (leader) {
+      tc_commit(&at_end[s]);
+      drain(&at_end[s], 0);
+    }
+    __syncwarp();
   } else if (warp < kSoftWarp0) {
     // ---- queries; V tiles: zero what no row sees, and what is not finite ----
     Piece q;
-    uint32_t base = 0, piece = 0;
+    uint32_t base = 0, piece = 0, copied = 0;  // copied: pieces whose queries have been asked for
     while (ok && walk.next(q)) {
       const int nt = q.t1 - q.t0;
       if (!kF32) {
         if (piece) wait(&q_free, (piece - 1) & 1);
+        copied += ok;
         if (ok && lane == 0) {
           mbar_arrive_expect_tx(&q_full, (q.pair ? 2 : 1) * L::kSlot);
           for (int r = 0; r < (q.pair ? 2 : 1); ++r)
@@ -585,6 +599,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       base += 2 * nt;
       ++piece;
     }
+    if (lane == 0 && copied) drain(&q_full, (copied - 1) & 1);
+    __syncwarp();
   } else {
     // ---- the two streams ----
     const int s = (warp - kSoftWarp0) >> 2, quad = warp & 3, row = 32 * quad + lane, st = tid - kSoftWarp0 * 32;
