@@ -608,10 +608,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const int G = 1 << p.g_shift;
     Piece q;
     uint32_t piece = 0, n_s = 0, n_o[2] = {0, 0};  // steps of this stream; of both, up to the piece's end
+    float scores = p.c;  // from this row's products to exponents of two
     int anc_of = -1;  // the request whose ancestors are in shared memory
-    // 32-bit queries of a piece into shared memory, in parts; rows behind its last zero
-    auto load_q = [&](const Piece& q) {
+    // 32-bit queries of a piece into shared memory, in parts; rows behind its last zero.  A row is taken times the power of
+    // two that brings its largest value to 2^13 (fp16: above 2^16 the first part is infinite, below 2^-3 the second loses
+    // bits) or 2^-20 (bf16: whose range the values of K may take up), and the inverse goes into the row's scale of scores,
+    // left in row_c for the row's threads.
+    auto load_q = [&](const Piece& q, float2* row_c) {
       constexpr int kPieces = D / 8;  // pieces of 8 values to a row
+      constexpr int kTop = kBf16 ? -20 : 13;
 #pragma unroll 4
       for (int e = st; e < kTile * kPieces; e += kSoft) {
         const int r = e / kPieces, c = e % kPieces, gr = q.row0 + r;
@@ -622,10 +627,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           x = __ldg(at);
           y = __ldg(at + 1);
         }
-        const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-        float rest[8];
+        float rest[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w}, top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) rest[i] = f[i];
+        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(rest[i]));
+#pragma unroll
+        for (int o = kPieces / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int exponent = (int)(__float_as_uint(top) >> 23);  // biased; a row of zeros or with an infinity stays as it is
+        const int up = top == 0.f || exponent == 255 ? 127 : max(1, min(253, 254 + kTop - exponent));
+        const float times = __uint_as_float((uint32_t)up << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rest[i] *= times;
+        if (c == 0) {
+          const float row = fminf(p.c * __uint_as_float((uint32_t)(254 - up) << 23), 3.4028234e38f);
+          row_c[r].x = row_c[kTile + r].x = row;
+        }
         uint8_t* to = smem + L::kQ + (c >> 3) * L::kBlock + r * 128 + (((c & 7) ^ (r & 7)) << 4);
 #pragma unroll
         for (int part = 0; part < L::kParts; ++part) {
@@ -647,7 +662,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         // Both product warps have passed the piece before: one without steps in it has no other tie to the streams, and
         // would miss a phase of q_full
         if (piece) wait(&q_free, (piece - 1) & 1);
-        load_q(q);
+        float2* row_c = s_ml + (piece & 1) * 2 * kTile;  // in the place of the maximum that this thread leaves at the piece's end
+        load_q(q, row_c);
+        named_bar_sync(1, kSoft);
+        scores = row_c[s * kTile + row].x;
       }
       const int nt = q.t1 - q.t0, steps = steps_of<L::kSingle>(q, s);
       const int row_item = (q.pair ? s * kTile : 0) + row, grow = q.row0 + row_item;  // row of the item; of the request and kv head
@@ -740,7 +758,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             top[1] = max3(top[1], __uint_as_float(v[w][e + 2]), __uint_as_float(v[w][e + 3]));
           }
         }
-        const float mx = max3(top[0], top[1], top[1]) * p.c;
+        const float mx = max3(top[0], top[1], top[1]) * scores;
         if (i == 0) {
           m = mx;
         } else if (__any_sync(0xffffffffu, !(mx <= m + kLag))) {
@@ -765,7 +783,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
         // an infinite maximum makes the row NaN
         const float off = m == -INFINITY ? kLift : m == INFINITY ? __int_as_float(0x7fffffff) : kLift - m;
-        const f32x2 c2 = pair(p.c, p.c), off2 = pair(off, off);
+        const f32x2 c2 = pair(scores, scores), off2 = pair(off, off);
         f32x2 sum[2] = {0, 0};
 #pragma unroll
         for (int w = 0; w < 2; ++w) {

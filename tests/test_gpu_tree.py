@@ -218,6 +218,76 @@ def test_pieces_of_one_tile_and_of_several_in_turn(q, kv, d, lens):
     c.check()
 
 
+def exact(c, scale=None):
+    """[nodes][heads][d] in 64 bits, of the nodes of requests"""
+    G, d, scale = c.heads // c.kv_heads, c.d, scale or c.d ** -0.5
+    out = torch.empty(c.N, c.heads, d, dtype=torch.float64, device="cuda")
+    for b in range(c.B):
+        n, a = c.n[b], int(c.start[b])
+        if n == 0:
+            continue
+        end, seen = c.lens[b] + n, c.seen(b).repeat_interleave(G, 0)
+        for h in range(c.kv_heads):
+            k, v = (torch.where(seen.any(0)[:, None], x[b, h, :end].double(), 0.0) for x in (c.k, c.v))
+            q = c.q[a:a + n, :c.heads * d].double().view(n, c.heads, d)[:, G * h:G * h + G].reshape(G * n, d)
+            p = torch.softmax((q @ k.T * scale).masked_fill(~seen, float("-inf")), 1)
+            out[a:a + n, G * h:G * h + G] = (p @ v).view(n, G, d)
+    return out[:int(c.start[-1])]
+
+
+def relative(c, want):
+    """L2 distance of the outputs relative to the result, the largest over (request, head)"""
+    got = c.out[:, :c.heads * c.d].double().view(c.N, c.heads, c.d)
+    worst = 0.0
+    for b in range(c.B):
+        rows = slice(int(c.start[b]), int(c.start[b + 1]))
+        if c.n[b]:
+            worst = max(worst, float(((got[rows] - want[rows]).square().sum((0, 2)) / want[rows].square().sum((0, 2))).max()) ** 0.5)
+    return worst
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kv", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [2.0 ** -140, 1e-30, 1e-6, 1e-4, 1e-3, 0.03, 100.0, 65520.0, 1e6, 1e30, 2.0 ** 125])
+def test_32_bit_queries_of_any_size(kv, d, size):
+    """With scale times size the same, a query of any size has the precision of one of ordinary size (bound as above)."""
+    c = Case([4, 9], [300, 70], 8, 2, d, q="f32", kv=kv, holes=0.05)
+    c.q = (c.q.double().clamp(-3.9, 3.9) * size).float()
+    scale = float(np.float32(min(d ** -0.5 / size, 2.0 ** 120)))
+    c.run(scale=scale)
+    assert c.status.item() == 0
+    assert relative(c, exact(c, scale)) <= 2.0 ** -19
+
+
+@pytest.mark.parametrize("kv", ["f16", "bf16"])
+def test_32_bit_queries_of_unlike_rows_and_values(kv):
+    """Rows from 1e-6 to 1e6 in one batch, and a value of 1e5 among ordinary ones that K has a zero for: a part of its row is off by
+    2^-38 of it at most, 2^-21 of an ordinary value."""
+    c = Case([16], [333], 4, 1, 128, q="f32", kv=kv)
+    c.q[:16] *= torch.logspace(-6, 6, 16, device="cuda")[:, None]
+    c.run()
+    c.check()
+    c = Case([16], [333], 4, 1, 128, q="f32", kv=kv)
+    c.q[:, ::128], c.k_at[..., 0] = 1e5, 0.0
+    c.run()
+    assert relative(c, exact(c)) <= 2.0 ** -19
+
+
+@pytest.mark.parametrize("kv", ["f16", "bf16"])
+def test_32_bit_queries_that_are_not_finite_or_zero(kv):
+    c = Case([6], [200], 4, 2, 64, q="f32", kv=kv, kind="star")
+    c.q[0] = 0.0
+    c.q[1, 5], c.q[2, 70], c.q[3, 130] = float("inf"), NAN, -float("inf")
+    c.q[4] *= 2.0 ** 17
+    c.run()
+    got = c.out[:6].view(6, 4, 64)
+    bad = torch.zeros(6, 4, dtype=torch.bool)
+    bad[1, 0] = bad[2, 1] = bad[3, 2] = True
+    assert torch.equal(torch.isnan(got).all(2).cpu(), bad) and torch.equal(torch.isnan(got).any(2).cpu(), bad)
+    mean = torch.stack([torch.cat([c.v[0, h, :200].double(), c.v[0, h, 200:201].double()]).mean(0) for h in (0, 0, 1, 1)])
+    assert ((got[0].double() - mean).abs() <= 2.0 ** -19 * c.v[0, :, :206].double().abs().amax()).all()
+
+
 def test_trees_that_begin_behind_other_nodes():
     """Nodes ahead of the first tree belong to nobody, whether items are cut between CTAs or not."""
     for lens in ([3000, 900], [5, 70]):
