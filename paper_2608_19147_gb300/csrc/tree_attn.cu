@@ -5,8 +5,11 @@
 // that share the kv head form one matrix Q (rows (node, head)), and
 //   O = softmax(scale Q K^T + visibility) V
 // is computed over tiles of 128 entries with a running maximum m and sum l per
-// row: S = Q K^T, P = 2^(S c - m), l += sum P, O += P V, all in tensor memory.  A
-// row sees a cache entry by the mask, a node's entry by its ancestor bits.
+// row: S = Q K^T, P = 2^((S - m) c), l += sum P, O += P V, all in tensor memory.  A
+// row sees a cache entry by the mask, a node's entry by its ancestor bits.  The maximum
+// is one of S itself: with a rounded product m c, S c - m c is off by half a step of it,
+// which makes weights overflow from 2^27 on (an addition more for two entries, 1.5 % of
+// the time of the trees of 64 below).
 //
 // Work split: an item is (request, kv head, up to 256 rows), its units the tiles
 // of entries; the units of all items, laid end to end, are cut into one equal run
@@ -64,6 +67,7 @@ constexpr int kSoft = 256;      // softmax threads
 // when it has been passed by 2^8: a weight is below 2^14, within fp16, and fp16
 // still holds weights 2^-20 of the largest with all its bits.
 constexpr float kLift = 6.f, kLag = 8.f;
+constexpr float kMost = 3.402823466e38f;  // the largest finite value
 
 struct Params {
   shard_tree_attn a;
@@ -72,9 +76,9 @@ struct Params {
   int g_shift;             // log2 of query heads per kv head
   int rows_max;            // rows of an item in `work`
   int act_order;
-  float c;                 // scale * log2(e)
+  float c;                 // scale * log2(e), finite
   int* plan;               // work: per request {first unit, first item, tiles, nodes}, then {all units, all items, CTAs, -}
-  float2* ml;              // work: [2 * CTAs][rows_max] maximum and sum
+  float4* ml;              // work: [2 * CTAs][rows_max] maximum, sum, and what scores are times
   float* o;                // work: [2 * CTAs][rows_max][D]
 };
 
@@ -617,8 +621,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     auto load_q = [&](const Piece& q, float2* row_c) {
       constexpr int kPieces = D / 8;  // pieces of 8 values to a row
       constexpr int kTop = kBf16 ? -20 : 13;
-#pragma unroll 4
-      for (int e = st; e < kTile * kPieces; e += kSoft) {
+      constexpr int kPass = kSoft / kPieces;  // rows at a time
+      const int passes = (q.rows + kPass - 1) / kPass;
+      int e = st;
+#pragma unroll 2
+      for (int pass = 0; pass < passes; ++pass, e += kSoft) {
         const int r = e / kPieces, c = e % kPieces, gr = q.row0 + r;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
         if (r < q.rows) {
@@ -638,7 +645,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < 8; ++i) rest[i] *= times;
         if (c == 0) {
-          const float row = fminf(p.c * __uint_as_float((uint32_t)(254 - up) << 23), 3.4028234e38f);
+          // (not 0, so that minus infinity stays; what is cut off is of scores below 2^-80)
+          const float row = fminf(fmaxf(p.c * __uint_as_float((uint32_t)(254 - up) << 23), 0x1p-126f), kMost);
           row_c[r].x = row_c[kTile + r].x = row;
         }
         uint8_t* to = smem + L::kQ + (c >> 3) * L::kBlock + r * 128 + (((c & 7) ^ (r & 7)) << 4);
@@ -653,6 +661,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           }
           *reinterpret_cast<uint4*>(to + part * L::kSlot) = make_uint4(w[0], w[1], w[2], w[3]);
         }
+      }
+#pragma unroll 1
+      for (; e < kTile * kPieces; e += kSoft) {
+        const int r = e / kPieces, c = e % kPieces;
+#pragma unroll
+        for (int part = 0; part < L::kParts; ++part)
+          *reinterpret_cast<uint4*>(smem + L::kQ + part * L::kSlot + (c >> 3) * L::kBlock + r * 128 + (((c & 7) ^ (r & 7)) << 4)) =
+              make_uint4(0, 0, 0, 0);
+        if (c == 0) row_c[r].x = row_c[kTile + r].x = p.c;
       }
       fence_async_proxy();
       mbar_arrive(&q_full);
@@ -716,7 +733,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         }
       };
       auto first_of = [&](int i) { return (q.t0 + (q.pair || L::kSingle ? i >> 1 : 2 * (i >> 1) + s)) * kTile + (i & 1) * kStep; };
-      float m = -INFINITY, l = 0.f;
+      float m = -kMost, l = 0.f;  // the score that weights are relative to (the lowest finite one until any is seen); their sum
       uint8_t mb[2];
       if (steps > 0) load_mask(first_of(0), mb);
 #pragma unroll 1
@@ -744,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         tc_ld32(S + 32, v[1]);
         tc_ld_wait(v[0]);
         tc_ld_wait(v[1]);
-        float top[2] = {-INFINITY, -INFINITY};
+        float top[2] = {-kMost, -kMost};
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           if (!__all_sync(0xffffffffu, see[w] == 0xffffffffu)) {
@@ -758,12 +775,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
             top[1] = max3(top[1], __uint_as_float(v[w][e + 2]), __uint_as_float(v[w][e + 3]));
           }
         }
-        const float mx = max3(top[0], top[1], top[1]) * scores;
+        const float mx = max3(top[0], top[1], top[1]);
+        const bool raise = !((mx - m) * scores <= kLag);  // or NaN
         if (i == 0) {
           m = mx;
-        } else if (__any_sync(0xffffffffu, !(mx <= m + kLag))) {
-          const bool raise = !(mx <= m + kLag);  // or NaN
-          const float f = raise ? exp2_fast(m - mx) : 1.f;
+        } else if (__any_sync(0xffffffffu, raise)) {
+          const float f = raise ? exp2_fast((m - mx) * scores) : 1.f;
           if (raise) m = mx;
           l *= f;
           wait_o(s, n_s - 1);
@@ -782,15 +799,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           tc_st_wait();
         }
         // an infinite maximum makes the row NaN
-        const float off = m == -INFINITY ? kLift : m == INFINITY ? __int_as_float(0x7fffffff) : kLift - m;
-        const f32x2 c2 = pair(scores, scores), off2 = pair(off, off);
+        const f32x2 c2 = pair(scores, scores), lift2 = pair(kLift, kLift), less2 = pair(-m, -m);
         f32x2 sum[2] = {0, 0};
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           uint32_t h[16], lo[16], least[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const f32x2 x = fma2(pair(__uint_as_float(v[w][2 * e]), __uint_as_float(v[w][2 * e + 1])), c2, off2);
+            const f32x2 x = fma2(add2(pair(__uint_as_float(v[w][2 * e]), __uint_as_float(v[w][2 * e + 1])), less2), c2, lift2);
             const float2 t = halves(x), y = make_float2(exp2_fast(t.x), exp2_fast(t.y));
             sum[e & 1] = add2(sum[e & 1], pair(y.x, y.y));
             h[e] = pack2<kBf16>(y.x, y.y);
@@ -823,8 +839,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       if (!q.pair) {
         const float2 x = ml[row], y = ml[kTile + row];
         M = both ? max3(x.x, y.x, y.x) : x.x;
-        w0 = x.x == M ? 1.f : exp2_fast(x.x - M);
-        w1 = !both ? 0.f : y.x == M ? 1.f : exp2_fast(y.x - M);
+        w0 = x.x == M ? 1.f : exp2_fast((x.x - M) * scores);
+        w1 = !both ? 0.f : y.x == M ? 1.f : exp2_fast((y.x - M) * scores);
         sum = both ? x.y * w0 + y.y * w1 : x.y;
       }
       const int steps_1 = steps_of<L::kSingle>(q, 1);
@@ -839,7 +855,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       const int c0 = q.pair ? 0 : s * (D / 2), c1 = q.pair ? D : c0 + D / 2;
       const bool odd = in_tree && s_odd[piece % (2 * L::kSlots)] == (int)piece + 1;
       const size_t slot = (2 * (size_t)blockIdx.x + (piece > 0)) * p.rows_max;  // of a piece of an item that is cut
-      if (!whole && row_item < q.rows && c0 == 0) p.ml[slot + row_item] = make_float2(M, sum);
+      if (!whole && row_item < q.rows && c0 == 0) p.ml[slot + row_item] = make_float4(M, sum, scores, 0.f);
       if (whole) {
         const float inv = 1.f / sum;
         w0 *= inv;
@@ -937,7 +953,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
 
-// Rows of items that were cut: sum_i 2^(m_i - M) O_i over sum_i 2^(m_i - M) l_i, the
+// Rows of items that were cut: sum_i 2^((m_i - M) c) O_i over sum_i 2^((m_i - M) c) l_i, the
 // pieces in order.  Bound by latency: the plan, then maxima and values together.  A warp per row of the batch (request,
 // kv head, node, head): with a grid of items by their most rows, CTAs for rows that are not there took 3 us for 16
 // requests of 5 nodes, and the join 17 us instead of 13 after 64 items of 256 rows.
@@ -989,10 +1005,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_combine_kernel(const __g
       else *reinterpret_cast<float2*>(v[i]) = __ldcg(reinterpret_cast<const float2*>(o));
     }
   };
-  float2 ml = make_float2(-INFINITY, 0.f);
+  float4 ml = make_float4(-kMost, 0.f, 0.f, 0.f);
   if (lane < n) ml = __ldcg(&p.ml[slot(lane)]);
   fetch(0);
   float M = ml.x;
+  const float scores = __shfl_sync(0xffffffffu, ml.z, 0);
   for (uint32_t i = lane + 32; i < n; i += 32) M = fmaxf(M, __ldcg(&p.ml[slot(i)]).x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
@@ -1003,8 +1020,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_combine_kernel(const __g
   for (uint32_t i0 = 0; i0 < n; i0 += kJoinPieces) {
     if (i0 > 0) fetch(i0);
     if (i0 % 32 == 0) {
-      if (i0 > 0) ml = i0 + lane < n ? __ldcg(&p.ml[slot(i0 + lane)]) : make_float2(-INFINITY, 0.f);
-      w = ml.x == M ? 1.f : exp2_fast(ml.x - M);
+      if (i0 > 0) ml = i0 + lane < n ? __ldcg(&p.ml[slot(i0 + lane)]) : make_float4(-kMost, 0.f, 0.f, 0.f);
+      w = ml.x == M ? 1.f : exp2_fast((ml.x - M) * scores);
       l = ml.y * w;
     }
 #pragma unroll
@@ -1058,7 +1075,7 @@ cudaError_t tree_attention_work(int N, int n_heads, int n_kv_heads, int head_dim
   int device;
   const cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
-  *bytes = kPlanBytes + 2ll * sms_of(device) * rows_of(N, n_heads / n_kv_heads) * (head_dim * 4 + 8);
+  *bytes = kPlanBytes + 2ll * sms_of(device) * rows_of(N, n_heads / n_kv_heads) * (head_dim * 4 + 16);
   return cudaSuccess;
 }
 
@@ -1075,12 +1092,12 @@ cudaError_t launch_tree_attention(const shard_tree_attn& a, bool act_order, cuda
   p.g_shift = G == 1 ? 0 : G == 2 ? 1 : G == 4 ? 2 : G == 8 ? 3 : 4;
   p.rows_max = rows_of(a.N, G);
   p.act_order = act_order;
-  p.c = a.scale * 1.44269504f;
+  p.c = std::min(a.scale * 1.44269504f, kMost);
   uint8_t* w = static_cast<uint8_t*>(a.work);
   const size_t rows = 2ull * sms * p.rows_max;
   p.plan = reinterpret_cast<int*>(w);
-  p.ml = reinterpret_cast<float2*>(w + kPlanBytes);
-  p.o = reinterpret_cast<float*>(w + kPlanBytes + rows * 8);
+  p.ml = reinterpret_cast<float4*>(w + kPlanBytes);
+  p.o = reinterpret_cast<float*>(w + kPlanBytes + rows * 16);
   // a dimension of one value may have any stride: one that the map takes
   const cuuint64_t dims[4] = {(cuuint64_t)a.head_dim, (cuuint64_t)a.capacity, (cuuint64_t)a.n_kv_heads, (cuuint64_t)a.B};
   const cuuint64_t entry = (cuuint64_t)a.kv_entry * 2;

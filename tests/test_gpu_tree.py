@@ -278,7 +278,7 @@ def test_32_bit_queries_that_are_not_finite_or_zero(kv):
     c = Case([6], [200], 4, 2, 64, q="f32", kv=kv, kind="star")
     c.q[0] = 0.0
     c.q[1, 5], c.q[2, 70], c.q[3, 130] = float("inf"), NAN, -float("inf")
-    c.q[4] *= 2.0 ** 17
+    c.q[4] *= 2.0 ** 120
     c.run()
     got = c.out[:6].view(6, 4, 64)
     bad = torch.zeros(6, 4, dtype=torch.bool)
@@ -320,6 +320,36 @@ def test_large_scores_and_weights_far_apart():
     c.q *= 100
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("q,kv,times", [("f16", "f16", 15000.0), ("bf16", "bf16", 2.0 ** 60), ("f32", "f16", 2.0 ** 110), ("f32", "bf16", 2.0 ** 55)])
+@pytest.mark.parametrize("P", [40, 300, 9000])
+def test_scores_beyond_what_32_bits_resolve(q, kv, times, P):
+    """Finite scores of 2^28 to 2^122: every row is its largest score's value, where the next is further below than 32 bits of the sum
+    of a score's products are off (d 2^-24 of |q| |k|)."""
+    c = Case([6], [P], 4, 2, 64, q=q, kv=kv)
+    c.q = (c.q.float().clamp(-4, 4) * times).to(c.q.dtype)
+    if kv == "f16":
+        c.k.clamp_(-4, 4).mul_(4000 if q == "f16" else 1)  # NaN stays
+    else:
+        c.k.mul_(2.0 ** 55)
+    c.run()
+    assert c.status.item() == 0
+    got, sure = c.out[:6].double().view(6, 2, 2, 64), 0
+    assert torch.isfinite(got).all()
+    for h in range(2):
+        seen = c.seen(0)
+        k, v = (torch.where(seen.any(0)[:, None], x[0, h, :P + 6].double(), 0.0) for x in (c.k, c.v))
+        for i in range(6):
+            for g in range(2):
+                qq = c.q[i].double().view(2, 2, 64)[h, g]
+                z, size = torch.where(seen[i], k @ qq, -torch.inf), (k.abs() @ qq.abs()).amax()
+                two = z.topk(2)
+                if two.values[0] - two.values[1] > 64 * 2.0 ** -23 * size:
+                    sure += 1
+                    assert ((got[i, h, g] - v[two.indices[0]]).abs() <= 2.0 ** -11 * v[two.indices[0]].abs() + 2.0 ** -24).all() if kv == "f16" else (
+                        (got[i, h, g] - v[two.indices[0]]).abs() <= 2.0 ** -8 * v[two.indices[0]].abs()).all()
+    assert sure >= 12
 
 
 def test_a_nodes_infinite_values_reach_only_those_that_see_it():
