@@ -320,7 +320,9 @@ enum {
  *               j * kv_entry values behind k (v); capacity entries each
  *   q_type, kv_type, out_type   SHARD_F32 (not kv_type), SHARD_F16, SHARD_BF16;
  *               16-bit queries have the cache's type.  Scores, softmax and sums
- *               are in 32 bits.  32-bit queries are used with 22 bits or more,
+ *               are in 32 bits; with 16-bit queries each weight is rounded to
+ *               the cache's type before it is multiplied with V (2^-11 of it at
+ *               most, bf16 2^-8).  32-bit queries are used with 22 bits or more,
  *               values below 2^-16 of the largest of their node and head to
  *               2^-38 of that
  *   mask        dev uint8 [B][mask_stride], mask_stride >= lens[b], or NULL

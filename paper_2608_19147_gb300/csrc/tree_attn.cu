@@ -31,13 +31,13 @@
 // tree's own entries that are not finite too; those are added to the rows that
 // see them when O is read.
 //
-// P is rounded to the cache's type for its product, 2^-9 (bf16) or 2^-12 of a
-// weight, as the values are; 32-bit queries and their P go as two parts of fp16 or
+// P is rounded to the cache's type for its product, 2^-8 (bf16) or 2^-11 of a
+// weight at most, as the values are; 32-bit queries and their P go as two parts of fp16 or
 // three of bf16, 22 or 24 bits, the small parts' products first (queries of 32 bits
 // on 500 to 900 entries: 5.5e-7 of the result off, with the large ones first 9e-7 and
 // 13e-7).  Three parts of P fit into tensor memory with one stream only (S, P and O of
-// two fill it): the second has no tiles then (252 us instead of 169 for fp16 on 95000
-// entries, 43 instead of 37 for 16 requests).
+// two fill it): the second has no tiles then (16-bit outputs: 278 us instead of 180 for
+// fp16 on 95000 entries, 48 instead of 40 for 16 requests).
 //
 // Measured (GB300, calls replayed): one node on 100 entries 9.2 us, 16 requests of
 // 5 nodes on 128 to 2048 entries 28.5 (65 MB), 4 trees of 64 at 64 / 8 heads on 4096
@@ -67,6 +67,14 @@ constexpr int kSoft = 256;      // softmax threads
 // when it has been passed by 2^8: a weight is below 2^14, within fp16, and fp16
 // still holds weights 2^-20 of the largest with all its bits.
 constexpr float kLift = 6.f, kLag = 8.f;
+// The tensor unit cuts the bits that a sum of 32 bits has no room for off, always toward zero: O loses some 2^-25 of
+// itself with each product added, 3e-5 over 64 tiles of three parts.  So O is taken over into a sum of its own, rounded to
+// nearest, after so many of a stream's tiles: one or two where both queries and outputs have 32 bits (error 5.4e-7 to 7e-7 of
+// the result on one to 256 tiles per CTA, 8.2e-7 with two, where it was 2.7e-5 after 64 and 1e-4 after 256), else where the
+// loss would come near the weights' rounding.  The sum is in tensor memory where that has room (head_dim 64; one stream,
+// whose sums the idle warps of the other take), else in `work`.  Times of two caches of 95000 entries, 32-bit queries and
+// outputs, without and with it: fp16 179 / 225 us (every tile 256), bf16 257 / 283; head_dim 64, fp16, 114 / 135; 5 nodes
+// instead of 32, fp16, 158 / 174.
 constexpr float kMost = 3.402823466e38f;  // the largest finite value
 
 struct Params {
@@ -80,6 +88,9 @@ struct Params {
   int* plan;               // work: per request {first unit, first item, tiles, nodes}, then {all units, all items, CTAs, -}
   float4* ml;              // work: [2 * CTAs][rows_max] maximum, sum, and what scores are times
   float* o;                // work: [2 * CTAs][rows_max][D]
+  float4* taken;           // work: [CTAs][2][taken_rows / 32][D / 4][32], a stream's O taken over (head_dim 128, two streams)
+  int taken_rows;          // rows of a stream at most, in whole warps
+  int fold;                // steps between two of these
 };
 
 // kRows: rows of an item at most.  128 where the requests have no more (or 32-bit queries take the second
@@ -91,6 +102,9 @@ struct Geo {
   static_assert(!kF32 || kRows == kTile, "the other tiles hold the lower parts");
   static constexpr int kParts = !kF32 ? 1 : kBf16 ? 3 : 2;  // of 11 or 8 bits of a 32-bit value
   static constexpr bool kSingle = kParts == 3;              // one stream: the other's S is where the third parts of P go
+  static constexpr bool kSpare = kSingle || D == 64;        // tensor memory has room for the sums that O is taken over into
+  // tiles of a stream from one to the next: 32-bit queries and outputs; else some 1000 products or 1500 (3e-5 to 5e-5)
+  static constexpr int kFold32 = kSpare ? 1 : 2, kFold = kParts == 1 ? 128 : 64;
   static constexpr int kQTiles = kF32 ? kParts : kRows / kTile;
   static constexpr uint32_t kBlock = kTile * 128;        // 64 columns of a tile of K, V or Q
   static constexpr uint32_t kSlot = kBlock * (D / 64);   // a tile
@@ -245,7 +259,58 @@ __device__ __forceinline__ int steps_of(const Piece& q, int s) {
   return 2 * todo - (todo > 0 && q.P + q.n - last * kTile <= kStep);
 }
 
-template <int D, bool kF32, bool kBf16, int kRows>
+// A row of O into the sum of those taken over, that times f, to the place of the one or the other.  Out of line: the loop
+// around it has no registers for this, which comes once in many steps; here all of a row's reads of `work` are on their way
+// together.
+template <int D, bool kSpare>
+__device__ __noinline__ void take_rows(uint32_t O, uint32_t T, float4* in_work, float f, bool there, bool first, bool back) {
+  if (kSpare) {
+#pragma unroll 1
+    for (int c = 0; c < D; c += 32) {
+      uint32_t x[32], t[32];
+      tc_ld32(O + c, x);
+      tc_ld32(T + c, t);
+      tc_ld_wait(x);
+      tc_ld_wait(t);
+      if (!first)
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(fmaf(__uint_as_float(t[e]), f, __uint_as_float(x[e])));
+      tc_st32((back ? O : T) + c, x);
+    }
+    tc_st_wait();
+    return;
+  }
+  constexpr int kHalf = D / 8;  // of a row's float4
+#pragma unroll 1
+  for (int h = 0; h < 2; ++h) {
+    float4 t[kHalf];
+#pragma unroll
+    for (int k = 0; k < kHalf; ++k) t[k] = there && !first ? __ldcg(in_work + 32 * (h * kHalf + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < kHalf / 4; ++c) {
+      uint32_t x[16];
+      tc_ld(O + 4 * h * kHalf + 16 * c, x);
+      tc_ld_wait(x);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float4& o = t[4 * c + k];
+        o = make_float4(fmaf(o.x, f, __uint_as_float(x[4 * k])), fmaf(o.y, f, __uint_as_float(x[4 * k + 1])),
+                        fmaf(o.z, f, __uint_as_float(x[4 * k + 2])), fmaf(o.w, f, __uint_as_float(x[4 * k + 3])));
+        x[4 * k] = __float_as_uint(o.x), x[4 * k + 1] = __float_as_uint(o.y), x[4 * k + 2] = __float_as_uint(o.z), x[4 * k + 3] = __float_as_uint(o.w);
+      }
+      if (back) tc_st16(O + 4 * h * kHalf + 16 * c, x);
+    }
+    if (there && !back)
+#pragma unroll
+      for (int k = 0; k < kHalf; ++k) __stcg(in_work + 32 * (h * kHalf + k), t[k]);
+    __syncwarp();
+  }
+  if (back) tc_st_wait();
+}
+
+// kTake: a stream's tiles may be more than p.fold.
+template <int D, bool kF32, bool kBf16, int kRows, bool kTake>
 __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __grid_constant__ Params p) {
   using L = Geo<D, kF32, kBf16, kRows>;
   constexpr uint32_t kIdescS = (1u << 4) | ((uint32_t)kBf16 << 7) | ((uint32_t)kBf16 << 10) | ((uint32_t)(kStep >> 3) << 17) |
@@ -258,10 +323,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
   // the V tiles) is safe; q_full, q_free: the piece's queries are in place, have been used by both streams;
   // s_full, p_ready, o_done: a step's S is computed, its P written, P V added (in turn for a stream's steps);
   // o_free: all have read a stream's O of a piece in which it has steps (a stream goes by its own pieces: one that
-  // counted the others' too would not follow the phases of those, and take an old one for the piece before); at_end:
-  // a stream's last product is done
+  // counted the others' too would not follow the phases of those, and take an old one for the piece before); o_full,
+  // o_taken: one stream's O is ready for the other's warps, has been taken over by them (a phase for each time: by o_done,
+  // which has one for each step, they would miss some); at_end: a stream's last product is done
   __shared__ uint64_t full[2 * L::kSlots], empty[L::kSlots], v_ready[L::kSlots], q_full, q_free, s_full[2][2], p_ready[2][2],
-      o_done[2][2], o_free[2], at_end[2];
+      o_done[2][2], o_free[2], o_full, o_taken, at_end[2];
   __shared__ uint32_t s_tmem;
   // pieces (counted from 1) whose tree entries hold a V that is not finite; V tiles run at most kSlots pieces ahead
   __shared__ volatile int s_odd[2 * L::kSlots];
@@ -290,6 +356,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       mbar_init(&q_free, 2);
       mbar_init(&o_free[0], 8);
       mbar_init(&o_free[1], 8);
+      mbar_init(&o_full, 1);
+      mbar_init(&o_taken, 4);
       mbar_init(&at_end[0], 1);
       mbar_init(&at_end[1], 1);
     }
@@ -441,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const uint32_t S = tmem + s * kTile, O = tmem + 2 * kTile + s * kTile;
     const uint32_t ring = smem_addr(smem + L::kRing);
     Piece q;
-    uint32_t base = 0, piece = 0, mine = 0, n = 0;  // first ring place of the piece; the stream's pieces and steps before it
+    uint32_t base = 0, piece = 0, mine = 0, taken = 0, n = 0;  // first ring place of the piece; before it the stream's pieces, its O's taken over, its steps
     while (ok && walk.next(q)) {
       const int nt = __shfl_sync(0xffffffffu, q.t1 - q.t0, 0), steps = __shfl_sync(0xffffffffu, steps_of<L::kSingle>(q, s), 0);
       const bool pair = __shfl_sync(0xffffffffu, (int)q.pair, 0), every = pair || L::kSingle;
@@ -462,6 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           const uint64_t V = smem_desc_sw128_mn(ring + slot_of(seq) * L::kSlot + half * (kStep * 128), L::kBlock);
           const int there = entries - (t0 + t) * kTile - half * kStep;  // entries from the step's first on
           if (i == 0 && mine) wait(&o_free[s], (mine - 1) & 1);
+          if (kTake && L::kSingle && i > 0 && (i & (p.fold - 1)) == 0) wait(&o_taken, taken++ & 1);
           if (!half) {
             wait(full_of(seq), full_turn(seq));
             wait(&v_ready[slot_of(nv)], turn_of(nv));
@@ -471,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           tc_fence_after();
           if (ok && leader) {
             auto add = [&](int x) {
-              const bool more = i > 0 || x > 0;
+              const bool more = (kTake ? i & (p.fold - 1) : i) != 0 || x > 0;
               if (L::kSingle) tc_mma(O, tmem + kTile + 32 * buf + 8 * x, V + ((x * 2048) >> 4), kIdescO, more);
               if (kF32) tc_mma(O, P + 32 * (x >> 1) + 16 + 8 * (x & 1), V + ((x * 2048) >> 4), kIdescO, L::kSingle || more);
               tc_mma(O, P + 32 * (x >> 1) + 8 * (x & 1), V + ((x * 2048) >> 4), kIdescO, kF32 || more);
@@ -484,6 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
               for (int x = 0; 16 * x < there; ++x) add(x);
             }
             tc_commit(&o_done[s][buf]);
+            if (kTake && L::kSingle && steps > p.fold && (((i + 1) & (p.fold - 1)) == 0 || i == steps - 1)) tc_commit(&o_full);
             if (half || i == steps - 1) release(slot_of(seq));
           }
           __syncwarp();
@@ -611,7 +681,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
     const uint32_t lanes = tmem + ((uint32_t)(32 * quad) << 16);
     const int G = 1 << p.g_shift;
     Piece q;
-    uint32_t piece = 0, n_s = 0, n_o[2] = {0, 0};  // steps of this stream; of both, up to the piece's end
+    uint32_t piece = 0, n_s = 0, n_o[2] = {0, 0}, n_full = 0;  // steps of this stream; of both, up to the piece's end; O's taken over from the other
     float scores = p.c;  // from this row's products to exponents of two
     int anc_of = -1;  // the request whose ancestors are in shared memory
     // 32-bit queries of a piece into shared memory, in parts; rows behind its last zero.  A row is taken times the power of
@@ -736,8 +806,39 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
       float m = -kMost, l = 0.f;  // the score that weights are relative to (the lowest finite one until any is seen); their sum
       uint8_t mb[2];
       if (steps > 0) load_mask(first_of(0), mb);
+      // This row's sum of O's taken over, and O, to the place of the one or the other: the sum is relative to the score
+      // taken_m, O to m_now.
+      const uint32_t O_own = lanes + 2 * kTile + (L::kSingle ? 0 : s * kTile), T_own = O_own + (D == 64 ? 64 : kTile);
+      float4* in_work = p.taken + ((size_t)(2 * blockIdx.x + s) * p.taken_rows + 32 * quad) * (D / 4) + lane;
+      float taken_m = 0.f;
+      auto take_over = [&](uint64_t* ready, uint32_t parity, auto&& m_of, bool first, bool back) {
+        wait(ready, parity);
+        __syncwarp();
+        tc_fence_after();
+        if (row_item - lane >= q.rows) return;  // nobody's rows
+        const float m_now = m_of(), f = taken_m == m_now ? 1.f : exp2_fast((taken_m - m_now) * scores);
+        taken_m = m_now;
+        take_rows<D, L::kSpare>(O_own, T_own, in_work, f, row_item < q.rows, first, back);
+        tc_fence_before();
+      };
+      float* s_m = reinterpret_cast<float*>(s_jump);  // [group of steps % 2][row]: one stream's m, for the other's warps
+      if (kTake && L::kSingle && s == 1) {
+        const int all = steps_of<L::kSingle>(q, 0);
+        if (all > p.fold)
 #pragma unroll 1
-      for (int i = 0; i < steps; ++i, ++n_s) {
+          for (int end = p.fold, group = 0;; end += p.fold, ++group) {
+            take_over(&o_full, n_full++ & 1, [&] { return s_m[group % 2 * kTile + row]; }, group == 0, end >= all);
+            __syncwarp();
+            if (end >= all) break;
+            if (lane == 0) mbar_arrive(&o_taken);
+          }
+      }
+#pragma unroll 1
+      for (int i = 0;; ++i, ++n_s) {
+        const bool fresh = kTake && (i & (p.fold - 1)) == 0;  // O begins anew
+        if (kTake && !L::kSingle && i > 0 && steps > p.fold && (fresh || i == steps))
+          take_over(&o_done[s][(n_s - 1) & 1], ((n_s - 1) >> 1) & 1, [&] { return m; }, i == p.fold, i == steps);
+        if (i >= steps) break;
         const int j0 = first_of(i);
         uint32_t see[2];
 #pragma unroll
@@ -783,20 +884,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
           const float f = raise ? exp2_fast((m - mx) * scores) : 1.f;
           if (raise) m = mx;
           l *= f;
-          wait_o(s, n_s - 1);
-          __syncwarp();
-          tc_fence_after();
-          const uint32_t O = lanes + 2 * kTile + s * kTile;
+          if (!fresh) {
+            wait_o(s, n_s - 1);
+            __syncwarp();
+            tc_fence_after();
 #pragma unroll 1
-          for (int w = 0; w < D / 16; ++w) {
-            uint32_t x[16];
-            tc_ld(O + 16 * w, x);
-            tc_ld_wait(x);
+            for (int w = 0; w < D / 16; ++w) {
+              uint32_t x[16];
+              tc_ld(O_own + 16 * w, x);
+              tc_ld_wait(x);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
-            tc_st16(O + 16 * w, x);
+              for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+              tc_st16(O_own + 16 * w, x);
+            }
+            tc_st_wait();
           }
-          tc_st_wait();
         }
         // an infinite maximum makes the row NaN
         const f32x2 c2 = pair(scores, scores), lift2 = pair(kLift, kLift), less2 = pair(-m, -m);
@@ -827,6 +929,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_attention_kernel(const __gri
         l += all.x + all.y;
         tc_st_wait();
         tc_fence_before();
+        if (kTake && L::kSingle && (((i + 1) & (p.fold - 1)) == 0 || i + 1 == steps)) s_m[(i & p.fold ? kTile : 0) + row] = m;
         __syncwarp();
         if (lane == 0) mbar_arrive(&p_ready[s][n_s & 1]);
       }
@@ -1051,22 +1154,36 @@ __global__ void __launch_bounds__(kJoinWarps * 32) tree_combine_kernel(const __g
 
 constexpr size_t kPlanBytes = (16 * (SHARD_MAX_TREES + 1) + 127) / 128 * 128;
 
-template <int D, bool kF32, bool kBf16, int kRows>
-cudaError_t launch(Params& p, int device, int grid, cudaStream_t s) {
+template <int D, bool kF32, bool kBf16, int kRows, bool kTake>
+cudaError_t launch_kernel(const Params& p, int device, int grid, cudaStream_t s) {
   using L = Geo<D, kF32, kBf16, kRows>;
   static std::atomic<uint64_t> ready{0};  // devices whose limit is raised
   if (device >= 64 || !(ready.load() >> device & 1)) {
-    const cudaError_t e = cudaFuncSetAttribute(tree_attention_kernel<D, kF32, kBf16, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    const cudaError_t e = cudaFuncSetAttribute(tree_attention_kernel<D, kF32, kBf16, kRows, kTake>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                (int)L::kTotal);
     if (e != cudaSuccess) return e;
     if (device < 64) ready.fetch_or(1ull << device);
   }
-  cudaError_t e = launch_behind(tree_attention_kernel<D, kF32, kBf16, kRows>, grid, kThreads, L::kTotal, s, p);
+  return launch_behind(tree_attention_kernel<D, kF32, kBf16, kRows, kTake>, grid, kThreads, L::kTotal, s, p);
+}
+
+// units: no fewer than there are
+template <int D, bool kF32, bool kBf16, int kRows>
+cudaError_t launch(Params& p, int device, int grid, long long units, cudaStream_t s) {
+  using L = Geo<D, kF32, kBf16, kRows>;
+  const int tiles = kF32 && p.a.out_type == SHARD_F32 ? L::kFold32 : L::kFold;
+  p.fold = 2 * tiles;
+  // A stream's tiles in a piece are no more than the cache's and than a CTA's.  Where they are within p.fold, the kernel
+  // without the code for more (without / with: one stream, two caches of 95000 entries, 257 / 278 us; trees of 64 on 60000
+  // entries 214 to 225 / 222 to 226).
+  const bool take = std::min<long long>((p.a.capacity + kTile - 1) / kTile, (units + grid - 1) / grid) > tiles;
+  cudaError_t e = take ? launch_kernel<D, kF32, kBf16, kRows, true>(p, device, grid, s) : launch_kernel<D, kF32, kBf16, kRows, false>(p, device, grid, s);
   if (e != cudaSuccess || grid < 2) return e;
   const long long rows = ((long long)p.a.N * p.a.n_kv_heads) << p.g_shift;
   return launch_behind(tree_combine_kernel<D>, dim3((unsigned)((rows + kJoinWarps - 1) / kJoinWarps)), kJoinWarps * 32, 0, s, p, kRows);
 }
 
+int taken_rows_of(int rows) { return std::min((rows + 31) / 32 * 32, kTile); }
 int rows_of(int N, int G) { return std::min(256, std::min(N, SHARD_MAX_TREE) * G); }
 
 }  // namespace
@@ -1075,7 +1192,8 @@ cudaError_t tree_attention_work(int N, int n_heads, int n_kv_heads, int head_dim
   int device;
   const cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
-  *bytes = kPlanBytes + 2ll * sms_of(device) * rows_of(N, n_heads / n_kv_heads) * (head_dim * 4 + 16);
+  const int rows = rows_of(N, n_heads / n_kv_heads);
+  *bytes = kPlanBytes + 2ll * sms_of(device) * (rows * (head_dim * 4ll + 16) + (head_dim == 64 ? 0 : taken_rows_of(rows) * (head_dim * 4ll)));
   return cudaSuccess;
 }
 
@@ -1098,6 +1216,8 @@ cudaError_t launch_tree_attention(const shard_tree_attn& a, bool act_order, cuda
   p.plan = reinterpret_cast<int*>(w);
   p.ml = reinterpret_cast<float4*>(w + kPlanBytes);
   p.o = reinterpret_cast<float*>(w + kPlanBytes + rows * 16);
+  p.taken = reinterpret_cast<float4*>(w + kPlanBytes + rows * (16 + 4ull * a.head_dim));
+  p.taken_rows = taken_rows_of(p.rows_max);
   // a dimension of one value may have any stride: one that the map takes
   const cuuint64_t dims[4] = {(cuuint64_t)a.head_dim, (cuuint64_t)a.capacity, (cuuint64_t)a.n_kv_heads, (cuuint64_t)a.B};
   const cuuint64_t entry = (cuuint64_t)a.kv_entry * 2;
@@ -1126,9 +1246,9 @@ cudaError_t launch_tree_attention(const shard_tree_attn& a, bool act_order, cuda
   if (units >= (1ll << 31)) return cudaErrorInvalidValue;
   const int grid = (int)std::min<long long>(sms, units);
 #define A(D)                                                                                                            \
-  if (f32) return bf ? launch<D, true, true, 128>(p, device, grid, s) : launch<D, true, false, 128>(p, device, grid, s); \
-  if (wide) return bf ? launch<D, false, true, 256>(p, device, grid, s) : launch<D, false, false, 256>(p, device, grid, s); \
-  return bf ? launch<D, false, true, 128>(p, device, grid, s) : launch<D, false, false, 128>(p, device, grid, s);
+  if (f32) return bf ? launch<D, true, true, 128>(p, device, grid, units, s) : launch<D, true, false, 128>(p, device, grid, units, s); \
+  if (wide) return bf ? launch<D, false, true, 256>(p, device, grid, units, s) : launch<D, false, false, 256>(p, device, grid, units, s); \
+  return bf ? launch<D, false, true, 128>(p, device, grid, units, s) : launch<D, false, false, 128>(p, device, grid, units, s);
   if (a.head_dim == 128) { A(128) }
   A(64)
 #undef A

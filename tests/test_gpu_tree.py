@@ -259,6 +259,60 @@ def test_32_bit_queries_of_any_size(kv, d, size):
     assert relative(c, exact(c, scale)) <= 2.0 ** -19
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kv", ["f16", "bf16"])
+@pytest.mark.parametrize("tiles,n", [(1, 5), (2, 5), (4, 5), (16, 5), (64, 5), (3, 64), (9, 50)])
+def test_32_bit_outputs_keep_their_precision_over_many_tiles(tiles, n, kv, d):
+    """152 items, each of so many tiles and by one CTA where the GPU has as many SMs: the precision of one tile (bound as above)."""
+    c = Case([n] * 19, [128 * tiles - n] * 19, 16, 8, d, q="f32", kv=kv, mask=False, seed=tiles, cap=128 * tiles)
+    c.run()
+    assert c.status.item() == 0
+    assert relative(c, exact(c)) <= 2.0 ** -19
+
+
+@pytest.mark.parametrize("q,kv,out", [("f16", "f16", "f16"), ("bf16", "bf16", "f32"), ("f32", "f16", "f16"), ("f32", "bf16", "bf16"), ("f32", "bf16", "f32"),
+                                      ("f32", "f16", "f32")])
+@pytest.mark.parametrize("n,d", [(2, 64), (2, 128), (40, 64), (20, 128)])
+def test_runs_of_long_and_short_pieces(q, kv, out, n, d):
+    """More items than SMs, of 133 tiles and of a few in turn, so that a CTA has several pieces, with more tiles than a stream adds up
+    before it takes its sums over and with fewer.  Relative to the result: half a step each for the weights (32-bit queries: 2^-19 as
+    above) and the outputs.  A tile left out or taken twice would be 2^-4."""
+    B = 40
+    c = Case([n, max(1, n // 2)] * (B // 2), [(17000, 300, 16800, 90, 700)[b % 5] for b in range(B)], 16, 4, d, q=q, kv=kv, out=out, holes=0.02)
+    c.run()
+    assert c.status.item() == 0
+    half = lambda t: torch.finfo(TYPES[t][0]).eps / 2  # noqa: E731
+    assert relative(c, exact(c)) <= (2.0 ** -19 if q == "f32" else half(kv)) + (0 if out == "f32" else half(out))
+
+
+@pytest.mark.parametrize("q,kv,out", [("f16", "f16", "f32"), ("bf16", "bf16", "f32"), ("f32", "f16", "f32"), ("f32", "f16", "f16"), ("f32", "bf16", "bf16")])
+@pytest.mark.parametrize("d", [64, 128])
+def test_sums_over_two_thousand_tiles(q, kv, out, d):
+    """All values 1, so that a result is 1 but for the sums: 1024 tiles a stream, and short pieces before them.  If the tensor unit cuts
+    off an ulp a product, of a sum that grows, n products lose n * 0.72 2^-23 / 2 of it: 3.5e-4 for all of them, 4.4e-5 for the 1024
+    that are added up before a sum is taken over (32-bit queries with 16-bit outputs: 1536, 6.6e-5, and the outputs' step).
+    Weights of 2^18 entries are rounded at random: 2^-9 / 2^9.  152 kv heads that overlap, and so do the two requests."""
+    heads, P = 152, 1 << 18
+    g = torch.Generator(device="cuda").manual_seed(7)
+    wide = d + 8 * heads
+    k = torch.randn(P + 3, wide, generator=g, device="cuda").to(TYPES[kv][0])
+    v = torch.ones_like(k)
+    x = torch.randn(3, heads * d, generator=g, device="cuda").to(TYPES[q][0])
+    o = torch.zeros(3, heads * d, device="cuda").to(TYPES[out][0])
+    start, parents, lens, status = (torch.tensor(a, dtype=torch.int32, device="cuda") for a in ([0, 1, 3], [-1, -1, 0], [300, P], [0]))
+    work = torch.empty(pkg.shard_tree_attention_work(3, heads, heads, d), dtype=torch.uint8, device="cuda")
+    pkg.shard_tree_attention(x.data_ptr(), TYPES[q][1], k.data_ptr(), v.data_ptr(), TYPES[kv][1], o.data_ptr(), TYPES[out][1], 2, 3, heads, heads, d,
+                             P + 2, (8, 8, wide), start.data_ptr(), parents.data_ptr(), lens.data_ptr(), None, 0, work.data_ptr(),
+                             work.numel(), status=status.data_ptr(), stream=torch.cuda.current_stream().cuda_stream)
+    assert status.item() == 0
+    step = 0 if out == "f32" else torch.finfo(TYPES[out][0]).eps / 2
+    off = (o.double() - 1).abs()
+    exact_sums = q == "f32" and out == "f32"
+    assert float(off[1:].mean()) <= step + (2.0 ** -19 if exact_sums else 2.0 ** -14)
+    assert float(off[1:].max()) <= step + (2.0 ** -18 if exact_sums else 2.0 ** -13)
+    assert float(off[0].max()) <= step + (2.0 ** -18 if q == "f32" else torch.finfo(TYPES[kv][0]).eps / 2)
+
+
 @pytest.mark.parametrize("kv", ["f16", "bf16"])
 def test_32_bit_queries_of_unlike_rows_and_values(kv):
     """Rows from 1e-6 to 1e6 in one batch, and a value of 1e5 among ordinary ones that K has a zero for: a part of its row is off by
