@@ -285,6 +285,21 @@ def test_runs_of_long_and_short_pieces(q, kv, out, n, d):
     assert relative(c, exact(c)) <= (2.0 ** -19 if q == "f32" else half(kv)) + (0 if out == "f32" else half(out))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("q,kv", [("f16", "f16"), ("bf16", "bf16"), ("f32", "f16"), ("f32", "bf16")])
+def test_every_tile_counts_once(q, kv, d):
+    """Queries of zero weigh all entries alike; a value is 1 in one column, another for each tile, so that a column is the share of its
+    tiles' entries that are seen: one tile more or less is a fourth of it or more.  Weights of 2^6 are exact."""
+    c = Case([4, 32, 1, 40], [20000, 33333, 7, 5000], 8, 2, d, q=q, kv=kv, out="f32", holes=0.05)
+    c.q.zero_()
+    tile = torch.arange(c.cap, device="cuda") // 128 % d
+    c.v.copy_(torch.where(torch.isfinite(c.v), torch.nn.functional.one_hot(tile, d).to(c.v.dtype), c.v))
+    c.run()
+    assert c.status.item() == 0
+    want, got = exact(c), c.out[:int(c.start[-1])].double().view(-1, 8, d)
+    assert ((got - want).abs() <= 2.0 ** -19 * want).all()
+
+
 @pytest.mark.parametrize("q,kv,out", [("f16", "f16", "f32"), ("bf16", "bf16", "f32"), ("f32", "f16", "f32"), ("f32", "f16", "f16"), ("f32", "bf16", "bf16")])
 @pytest.mark.parametrize("d", [64, 128])
 def test_sums_over_two_thousand_tiles(q, kv, out, d):
@@ -340,6 +355,15 @@ def test_32_bit_queries_that_are_not_finite_or_zero(kv):
     assert torch.equal(torch.isnan(got).all(2).cpu(), bad) and torch.equal(torch.isnan(got).any(2).cpu(), bad)
     mean = torch.stack([torch.cat([c.v[0, h, :200].double(), c.v[0, h, 200:201].double()]).mean(0) for h in (0, 0, 1, 1)])
     assert ((got[0].double() - mean).abs() <= 2.0 ** -19 * c.v[0, :, :206].double().abs().amax()).all()
+
+
+@pytest.mark.parametrize("q,kv", [("f16", "f16"), ("bf16", "bf16"), ("f32", "f16"), ("f32", "bf16")])
+def test_long_cache_split_and_joined_has_the_precision_of_a_short_one(q, kv):
+    """Relative to the result, per request and head: half a step each for the weights and the outputs (32-bit queries 2^-19 as above),
+    however long the cache; 128 entries left out of 33333 would be 2^-4."""
+    c = Case([4, 32, 1], [20000, 33333, 7], 8, 2, 128, q=q, kv=kv, holes=0.05)
+    c.run()
+    assert relative(c, exact(c)) <= (2.0 ** -19 if q == "f32" else torch.finfo(TYPES[kv][0]).eps)
 
 
 def test_trees_that_begin_behind_other_nodes():
