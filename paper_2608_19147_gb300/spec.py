@@ -24,8 +24,8 @@ from typing import Callable, List, Optional, Sequence, Tuple
 
 import numpy as np
 
-from . import (SHARD_MAX_TOKENS, SHARD_MAX_TREE, SHARD_MAX_TREE_NODES, head_sample, head_top1_host, kv_state_alloc, kv_state_free, shard_prefill,
-               shard_step_host, shard_step_tree, shard_sync_status, shard_tree_accept)
+from . import (SHARD_MAX_REQUESTS, SHARD_MAX_TOKENS, SHARD_MAX_TREE, SHARD_MAX_TREE_NODES, head_sample, head_top1_host, kv_state_alloc, kv_state_free,
+               kv_state_length, kv_trim, shard_prefill, shard_step_host, shard_step_tree, shard_sync_status, shard_tree_accept)
 
 # forward(token_ids [n] int32, position_ids [n] int32, mask [L + n] uint8) -> greedy tokens [n] int32
 Forward = Callable[[np.ndarray, np.ndarray, np.ndarray], np.ndarray]
@@ -179,16 +179,28 @@ class TreeDecoder:
     every node of the kept path makes the emitted tokens draws of the model,
     whatever was drafted; with temperature 0 they are the greedy tokens.
 
-    stages, hidden, head as in ShardPipeline; settings: temperature, top_k, top_p
-    and min_p of all requests; draws(n) gives n random numbers in [0, 1)."""
+    Every node of a step keeps its entry of the cache, kept or not (the rewind is
+    a mask), so `capacity` counts all nodes that are ever verified.
+
+    stages, hidden, head as in ShardPipeline; B at most SHARD_MAX_REQUESTS;
+    settings: temperature, top_k, top_p and min_p of all requests; draws(n) gives
+    n random numbers in [0, 1).  Where the head has no token for a request
+    (logits that are not numbers, draws out of range, or a device wait that gave
+    up, after which the head is to be created again), prefill and step raise
+    RuntimeError and leave the decoder as it was before."""
 
     def __init__(self, stages: Sequence[int], hidden: int, head: int, B: int, capacity: int, temperature: float = 1.0,
                  top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0, draws: Optional[Callable[[int], np.ndarray]] = None):
+        t, p, low = np.float32(temperature), np.float32(top_p), np.float32(min_p)
+        if not (0 <= t < np.inf and top_k >= 0 and 0 < p <= 1 and 0 <= low <= 1):
+            raise ValueError("temperature %r, top_k %r, top_p %r or min_p %r out of range" % (temperature, top_k, top_p, min_p))
+        if not 1 <= B <= SHARD_MAX_REQUESTS:
+            raise ValueError("%d requests outside [1, %d]" % (B, SHARD_MAX_REQUESTS))
         import torch
 
         self.torch = torch
         self.stages, self.hidden, self.head, self.B, self.capacity = list(stages), hidden, head, B, capacity
-        self.states = [kv_state_alloc(s, B, capacity) for s in self.stages]
+        self.states: List[int] = []
         self.mask = torch.zeros((B, capacity), dtype=torch.uint8, device="cuda")
         self.length = [0] * B    # entries, kept or not
         self.position = [0] * B  # of the current token
@@ -200,6 +212,12 @@ class TreeDecoder:
                              top_k=torch.full((n,), int(top_k), dtype=torch.int32, device="cuda"),
                              top_p=torch.full((n,), float(top_p), device="cuda"),
                              min_p=torch.full((n,), float(min_p), device="cuda"))
+        try:
+            for sh in self.stages:
+                self.states.append(kv_state_alloc(sh, B, capacity))
+        except Exception:
+            self.close()
+            raise
 
     def _dev(self, values, dtype):
         return self.torch.from_numpy(np.ascontiguousarray(values, dtype=dtype)).to("cuda")
@@ -214,16 +232,30 @@ class TreeDecoder:
                         **{k: v.data_ptr() for k, v in self.settings.items()}, stream=stream)
         return token
 
+    def _require(self, tokens: Sequence[Sequence[int]]) -> None:
+        """Where a request has no token: its and all others' entries behind the lengths taken back, and an error."""
+        bad = [b for b, t in enumerate(tokens) if any(x < 0 for x in t)]
+        if not bad:
+            return
+        for st in self.states:
+            for b in range(self.B):
+                n = kv_state_length(st, b)
+                if n > self.length[b]:
+                    kv_trim(st, b, np.arange(n) < self.length[b])
+        raise RuntimeError("head %d has no token for request %s: logits that are not numbers, draws outside [0, 1), or a device wait that "
+                           "gave up" % (self.head, ", ".join(map(str, bad))))
+
     def prefill(self, prompts: Sequence[Sequence[int]]) -> List[int]:
         """Runs each request's prompt through the stages; the first generated token of each."""
         if len(prompts) != self.B or any(len(p) == 0 for p in prompts):
             raise ValueError("one prompt of at least one token for each request")
+        for b, prompt in enumerate(prompts):
+            if self.length[b] + len(prompt) > self.capacity:
+                raise ValueError("request %d would hold %d entries > %d" % (b, self.length[b] + len(prompt), self.capacity))
         torch, stream = self.torch, self.torch.cuda.current_stream().cuda_stream
         last = torch.empty((self.B, self.hidden), dtype=torch.int16, device="cuda")
         for b, prompt in enumerate(prompts):
             n, at = len(prompt), self.length[b]
-            if at + n > self.capacity:
-                raise ValueError("request %d would hold %d entries > %d" % (b, at + n, self.capacity))
             ids, pos = self._dev(prompt, np.int32), self._dev(np.arange(self.position[b], self.position[b] + n), np.int32)
             self.mask[b, at:at + n] = 1
             h = None
@@ -233,13 +265,16 @@ class TreeDecoder:
                               self.mask[b].data_ptr(), self.capacity, out.data_ptr(), stream)
                 h = out
             last[b] = h[n - 1]
-            self.length[b] += n
-            self.position[b] += n
         token = self._sample(last, self.B)
         for sh in self.stages:
             shard_sync_status(sh, stream)
-        self.current = token.tolist()
-        return list(self.current)
+        first = token.tolist()
+        self._require([[t] for t in first])
+        for b, prompt in enumerate(prompts):
+            self.length[b] += len(prompt)
+            self.position[b] += len(prompt)
+        self.current = first
+        return list(first)
 
     def step(self, trees: Optional[Sequence[Tuple[Sequence[int], Sequence[int]]]] = None) -> List[List[int]]:
         """Verifies one tree per request, (drafts, parents) each, or decodes plainly (None); the emitted tokens of each."""
@@ -281,6 +316,7 @@ class TreeDecoder:
             shard_sync_status(sh, stream)
         kept, tok = count.tolist(), emitted.tolist()
         out = [tok[b][:kept[b]] for b in range(self.B)]
+        self._require(out)
         for b in range(self.B):
             self.length[b] += n[b]
             self.position[b] += kept[b]

@@ -278,3 +278,34 @@ def test_decoder_refuses(model):
         assert len(d.step([([5, 6], [0, 0])])[0]) in (1, 2)
     finally:
         d.close()
+
+
+def test_a_request_without_a_token_is_an_error_and_changes_nothing(model):
+    """Draws that are no numbers: prefill and step raise, and the decoder goes on as one that never had them."""
+    stages, head = model
+    nan, trees = (lambda n: np.full(n, np.nan)), [([7, 8, 9], [0, 0, 1]), ([5], [0]), ((), ())]
+    outs = []
+    for spoil in (False, True):
+        d = TreeDecoder(stages, synth.TINY.hidden, head, len(PROMPTS), 60, temperature=0.8, draws=lambda n: np.full(n, 0.4))
+        try:
+            good, out = d.draws, []
+
+            def call(f, *a):
+                if spoil:
+                    d.draws = nan
+                    with pytest.raises(RuntimeError, match="request 0, 1, 2"):
+                        f(*a)
+                    d.draws = good
+                out.append(f(*a))
+
+            with pytest.raises(ValueError):
+                d.prefill(PROMPTS[:2] + [[1] * 61])
+            call(d.prefill, PROMPTS)
+            for _ in range(3):
+                call(d.step, trees)
+            for st in d.states:
+                assert [pkg.kv_state_length(st, b) for b in range(3)] == d.length
+            outs.append((out, d.length, d.position))
+        finally:
+            d.close()
+    assert outs[0] == outs[1]

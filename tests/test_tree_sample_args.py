@@ -72,3 +72,12 @@ def test_tree_depths():
     for bad in ([0], [-1, 1], [-1, -1], [-1, 0, 5]):
         with pytest.raises(ValueError):
             tree_depths(bad)
+
+
+def test_decoder_settings():
+    from paper_2608_19147_gb300.spec import TreeDecoder
+
+    for bad in (dict(temperature=-0.1), dict(temperature=float("inf")), dict(temperature=float("nan")), dict(top_k=-1), dict(top_p=0.0), dict(top_p=1.1),
+                dict(top_p=1e-50), dict(min_p=-0.1), dict(min_p=1.1), dict(B=0), dict(B=pkg.SHARD_MAX_REQUESTS + 1)):
+        with pytest.raises(ValueError):
+            TreeDecoder([], 64, P, **{"B": 1, "capacity": 16, **bad})
