@@ -1240,8 +1240,9 @@ cudaError_t launch_tree_attention(const shard_tree_attn& a, bool act_order, cuda
   // Items of 256 rows where the requests have more than 128 on the whole: half the reads of a cache that L2 does not hold
   // (256 / 128: two trees of 64 with 8 heads to a kv head on 60000 entries 219 / 301 us, on 4096 entries 54 / 55; 128 rows
   // on 95000 entries 141 / 131, for the slot less).
-  const bool f32 = a.q_type == SHARD_F32, bf = a.kv_type == SHARD_BF16, wide = !f32 && (long long)a.N * G > 128ll * a.B;
-  const long long items = a.n_kv_heads * ((long long)std::min(a.B, a.N) + (long long)a.N * G / (wide ? 256 : 128));
+  const long long nodes = std::min<long long>(a.N, (long long)a.B * SHARD_MAX_TREE);  // of trees; the others are nobody's
+  const bool f32 = a.q_type == SHARD_F32, bf = a.kv_type == SHARD_BF16, wide = !f32 && nodes * G > 128ll * a.B;
+  const long long items = a.n_kv_heads * ((long long)std::min(a.B, a.N) + nodes * G / (wide ? 256 : 128));
   const long long units = items * ((a.capacity + kTile - 1) / kTile);
   if (units >= (1ll << 31)) return cudaErrorInvalidValue;
   const int grid = (int)std::min<long long>(sms, units);

@@ -491,6 +491,27 @@ def test_bad_parents_count_as_none():
     c.check()
 
 
+def test_many_more_nodes_than_the_trees_have():
+    """Nodes behind the last tree count for nothing: a buffer of 2^20 of them with one small tree on a cache of 2^23 entries."""
+    t = torch.Generator(device="cuda").manual_seed(1)
+    N, G, d, cap = 1 << 20, 16, 64, 1 << 23
+    kv = torch.empty(cap, d, dtype=torch.float16, device="cuda")
+    kv[:200] = torch.randn(200, d, generator=t, device="cuda").half()
+    start, parents, lens = (torch.tensor(a, dtype=torch.int32, device="cuda") for a in ([0, 3], [-1, 0, 0], [190]))
+    parents = torch.cat([parents, torch.full((N - 3,), -1, dtype=torch.int32, device="cuda")])
+    q = torch.zeros(N, G * d, dtype=torch.float16, device="cuda")
+    q[:3] = torch.randn(3, G * d, generator=t, device="cuda").half()
+    outs = []
+    for n in (3, N):
+        out = torch.full((n, G * d), 7.0, dtype=torch.float16, device="cuda")
+        work = torch.empty(pkg.shard_tree_attention_work(n, G, 1, d), dtype=torch.uint8, device="cuda")
+        pkg.shard_tree_attention(q.data_ptr(), pkg.SHARD_F16, kv.data_ptr(), kv.data_ptr(), pkg.SHARD_F16, out.data_ptr(), pkg.SHARD_F16, 1, n, G, 1, d,
+                                 cap, (cap * d, cap * d, d), start.data_ptr(), parents.data_ptr(), lens.data_ptr(), None, 0, work.data_ptr(), work.numel(),
+                                 stream=torch.cuda.current_stream().cuda_stream)
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1][:3]) and (outs[1][3:] == 7).all() and (outs[0] != 7).all()
+
+
 def test_refusals():
     c = Case([2], [9], 4, 2, 64)
     E, U = pkg.SHARD_EINVAL, pkg.SHARD_EUNSUPPORTED
