@@ -90,8 +90,11 @@ int head_top1_host(head_t head, const uint16_t* hidden, int M, int32_t* token, f
  * ids, exceed u times the sum of all that are kept.  T = 0 is the greedy token.
  * Every array is dev [M], one value per row, or NULL: T 1, top_k 0, top_p 1,
  * min_p 0; u must be given.
- * Weights have 28 bits or more and are summed exactly, so that a row's token
- * depends on nothing but the row.  Logits of minus infinity and NaN are never
+ * A weight is a whole number of 2^-44 of the largest, off by half of that and
+ * 2^-28 of itself at most (so p of a token of 2^-30 has 14 bits), and sums are
+ * exact, so that a row's token depends on nothing but the row.  A token below
+ * 2^-45 of the largest is never drawn, though it counts in n_kept where no
+ * filter drops it.  Logits of minus infinity and NaN are never
  * chosen; infinite logits are equally likely and exclude all others.  A row
  * with no token to choose from, or with T < 0 or not finite, top_k < 0, top_p
  * outside (0, 1], min_p outside [0, 1] or u outside [0, 1), has token -1, p NaN
@@ -120,7 +123,8 @@ int head_sample_logits(const void* logits, int type, int M, int V, long long ld,
 /* head_top1 with sampling: draws a token for each of M hidden rows (1 <= M <=
  * SHARD_MAX_TOKENS) from the head's logits.  A bounded device wait of the
  * projection that gave up (never expected) makes every row's token -1, as in
- * head_top1.  Errors: EINVAL, ECUDA. */
+ * head_top1.  Errors: EINVAL, EUNSUPPORTED (vocab > HEAD_MAX_SAMPLE_VOCAB),
+ * ECUDA. */
 int head_sample(head_t head, const uint16_t* hidden, int M, const head_sampling* sampling, int32_t* token, float* p,
                 int32_t* n_kept, void* cuda_stream);
 
