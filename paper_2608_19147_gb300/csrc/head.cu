@@ -475,6 +475,8 @@ int head_sample(head_t h, const uint16_t* hidden, int M, const head_sampling* sa
                 int32_t* n_kept, void* cuda_stream) {
   if (!h || !hidden || !sampling || !sampling->u || !token) return fail(SHARD_EINVAL, "head_sample: null argument");
   if (M < 1 || M > SHARD_MAX_TOKENS) return fail(SHARD_EINVAL, "head_sample: M = %d outside [1, %d]", M, SHARD_MAX_TOKENS);
+  if (reinterpret_cast<uintptr_t>(hidden) % 2 || !sampling_aligned(*sampling, token, p, n_kept))
+    return fail(SHARD_EINVAL, "head_sample: an array is not aligned to its values");
   if (h->cfg.vocab > HEAD_MAX_SAMPLE_VOCAB)
     return fail(SHARD_EUNSUPPORTED, "head_sample: vocab %d > %d", h->cfg.vocab, HEAD_MAX_SAMPLE_VOCAB);
   HEAD_CUDA_TRY(cudaSetDevice(h->device));

@@ -27,6 +27,12 @@ cudaError_t launch_behind(void (*kern)(Params...), dim3 grid, dim3 block, size_t
   return cudaLaunchKernelEx(&cfg, kern, std::forward<Args>(args)...);
 }
 
+// Whether pointers are aligned to values of 4 bytes (null ones are).
+template <class... P>
+bool aligned4(const P*... p) {
+  return (((reinterpret_cast<uintptr_t>(p)) | ...) & 3) == 0;
+}
+
 // SMs of a device (0: unknown).
 inline int sms_of(int device) {
   static std::atomic<int> known[64];

@@ -968,6 +968,10 @@ cudaError_t launch_type(SampleArgs a, int M, int sms, cudaStream_t s) {
 
 namespace shard {
 
+bool sampling_aligned(const head_sampling& s, const int32_t* token, const float* p, const int32_t* n_kept) {
+  return aligned4(s.temperature, s.top_k, s.top_p, s.min_p, s.u, token, p, n_kept);
+}
+
 cudaError_t launch_sample(const void* logits, int type, int M, int V, long long ld, const head_sampling& s, int32_t* token,
                           float* p, int32_t* n_kept, const int* failed, int sms, cudaStream_t stream) {
   const SampleArgs a{logits, V, 0, ld, s, token, p, n_kept, failed};
@@ -986,6 +990,8 @@ extern "C" int head_sample_logits(const void* logits, int type, int M, int V, lo
   if (M < 1 || V < 1 || ld < V) return fail(SHARD_EINVAL, "head_sample_logits: M %d, V %d or ld %lld out of range", M, V, ld);
   if (reinterpret_cast<uintptr_t>(logits) % (type == SHARD_F32 ? 4 : 2))
     return fail(SHARD_EINVAL, "head_sample_logits: logits is not aligned to its values");
+  if (!sampling_aligned(*sampling, token, p, n_kept))
+    return fail(SHARD_EINVAL, "head_sample_logits: an array is not aligned to its values");
   if (V > HEAD_MAX_SAMPLE_VOCAB || M > HEAD_MAX_SAMPLE_ROWS)
     return fail(SHARD_EUNSUPPORTED, "head_sample_logits: V %d > %d or M %d > %d", V, HEAD_MAX_SAMPLE_VOCAB, M, HEAD_MAX_SAMPLE_ROWS);
   OnDeviceOf on(logits);

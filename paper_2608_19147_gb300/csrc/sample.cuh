@@ -41,6 +41,9 @@ __device__ __constant__ const float2 kSampleTable[64] = {
     {0x1.f50766p+0f, -0x1.246ebp-26f}, {0x1.fa7c18p+0f, 0x1.9e90d8p-28f},
 };
 
+// Whether a call's arrays are aligned to their values.
+bool sampling_aligned(const head_sampling& s, const int32_t* token, const float* p, const int32_t* n_kept);
+
 // Samples M rows of logits (arguments checked by the caller); rows get token -1
 // where *failed (dev, or null) is not zero.  On the current device, of `sms` SMs.
 cudaError_t launch_sample(const void* logits, int type, int M, int V, long long ld, const head_sampling& s,

@@ -13,6 +13,7 @@
 #include "../../include/shard.h"
 #include "../../include/shard_debug.h"
 #include "common.cuh"
+#include "launch.cuh"
 #include "tree.cuh"
 
 using namespace shard;
@@ -1106,6 +1107,8 @@ int shard_step_tree(shard_t sh, kvstate_t st, const uint16_t* hidden_in, const i
   if (B != st->n_rows || B > kMaxRequests)
     return fail(SHARD_EINVAL, "shard_step_tree: B (%d) must equal the state's n_rows (%d) and be at most %d", B, st->n_rows,
                 kMaxRequests);
+  if (reinterpret_cast<uintptr_t>(hidden_in) % 2 || reinterpret_cast<uintptr_t>(hidden_out) % 2 || !aligned4(token_ids, parents, position_ids))
+    return fail(SHARD_EINVAL, "shard_step_tree: an array is not aligned to its values");
   const int G = sh->Hq / sh->Hkv;
   if (G & (G - 1)) return fail(SHARD_EUNSUPPORTED, "shard_step_tree: %d query heads per kv head (supported: 1, 2, 4, 8, 16)", G);
   if (st->poisoned) return fail(SHARD_EINVAL, "shard_step_tree: the KV state was left inconsistent; reset it");

@@ -126,6 +126,8 @@ int shard_tree_attention(const shard_tree_attn* args, void* cuda_stream) {
   if ((bits(a.q) | bits(a.k) | bits(a.v) | bits(a.out) | bits(a.work)) % 16 || a.q_stride * q_size % 16 ||
       a.out_stride * out_size % 16 || a.kv_request % 8 || a.kv_head % 8 || a.kv_entry % 8)
     return fail(SHARD_EINVAL, "shard_tree_attention: a pointer or stride is not a multiple of 16 bytes");
+  if (!aligned4(a.tree_start, a.parents, a.lens, a.status))
+    return fail(SHARD_EINVAL, "shard_tree_attention: an int32 array is not aligned to its values");
   if (a.scale == 0.f) a.scale = 1.f / sqrtf((float)a.head_dim);
   if (!(a.scale > 0.f && a.scale < INFINITY)) return fail(SHARD_EINVAL, "shard_tree_attention: scale %g", (double)a.scale);
   if ((a.n_kv_heads > 1 && !a.kv_head) || (a.B > 1 && !a.kv_request))
@@ -155,6 +157,8 @@ int shard_tree_accept(int B, int N, const int32_t* tree_start, const int32_t* pa
   if (B < 1 || B > SHARD_MAX_TREES || N < 1 || path_stride < 1 || (attention_mask && mask_stride < 1))
     return fail(SHARD_EINVAL, "shard_tree_accept: B %d (1..%d), N %d, path_stride %d or mask_stride %d out of range", B,
                 SHARD_MAX_TREES, N, path_stride, mask_stride);
+  if (!aligned4(tree_start, parents, drafts, targets, path, tokens, count, lens, status))
+    return fail(SHARD_EINVAL, "shard_tree_accept: an int32 array is not aligned to its values");
   OnDeviceOf on(parents);
   if (on.error()) return fail(SHARD_EINVAL, "shard_tree_accept: parents is not device memory");
   tree_accept_kernel<<<B, SHARD_MAX_TREE, 0, static_cast<cudaStream_t>(cuda_stream)>>>(

@@ -167,6 +167,24 @@ def test_tree_step_refusals_and_guards(tiny):
         g.close()
 
 
+def test_tree_step_refuses_arrays_that_are_not_aligned_to_their_values(tiny):
+    w, sh = tiny
+    g = GpuEngine(sh, 2, 64)
+    try:
+        dev = [to_dev(np.asarray(x, np.int32)) for x in ([-1, 0, -1, 0], [0, 1, 0, 0])] + [to_dev(np.ones((2, 64), np.uint8))]
+        dev += [to_dev(synth.hidden_in(synth.TINY, SEED, 1, 4)), torch.empty((4, synth.TINY.hidden), dtype=torch.int16, device="cuda")]
+        p = [x.data_ptr() for x in dev]
+        good = dict(hidden_in=p[3], token_ids=None, n_new=[2, 1], parents=p[0], position_ids=p[1], attention_mask=p[2], mask_stride=64, hidden_out=p[4])
+        for over in (dict(parents=p[0] + 2), dict(position_ids=p[1] + 1), dict(hidden_in=p[3] + 1), dict(hidden_out=p[4] + 1),
+                     dict(hidden_in=None, token_ids=p[0] + 2)):
+            assert pkg.shard_step_tree(g.shard.h, g.st, **{**good, **over}, stream=g.stream, check=False) == pkg.SHARD_EINVAL, over
+            assert "aligned" in pkg.shard_last_error()
+        pkg.shard_step_tree(g.shard.h, g.st, **{**good, "hidden_in": p[3] + 2}, stream=g.stream)  # to its values is enough
+        pkg.shard_sync_status(g.shard.h, g.stream)
+    finally:
+        g.close()
+
+
 def test_a_request_does_not_see_the_others(tiny):
     w, sh = tiny
     shape = synth.TINY

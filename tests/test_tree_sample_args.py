@@ -36,6 +36,18 @@ def test_attention_does_not_support(over):
     assert "shard_tree_attention" in pkg.shard_last_error()
 
 
+def test_arrays_that_are_not_aligned_to_their_values():
+    for name in ("tree_start", "parents", "lens", "status"):
+        assert attention(**{name: P + 2}) == pkg.SHARD_EINVAL and "shard_tree_attention: an int32" in pkg.shard_last_error()
+    good = dict(B=1, N=4, tree_start=P, parents=P, drafts=P, targets=P, path_stride=4, path=P, tokens=P, count=P)
+    for name in ("tree_start", "parents", "drafts", "targets", "path", "tokens", "count", "status"):
+        assert pkg.shard_tree_accept(**{**good, name: P + 1}, check=False) == pkg.SHARD_EINVAL and "aligned" in pkg.shard_last_error()
+    assert pkg.shard_tree_accept(**good, lens=P + 2, attention_mask=P + 1, mask_stride=9, check=False) == pkg.SHARD_EINVAL
+    good = dict(logits=P, type=pkg.SHARD_F32, M=1, V=8, ld=8, u=P, token=P)
+    for name in ("u", "token", "temperature", "top_k", "top_p", "min_p", "p", "n_kept"):
+        assert pkg.head_sample_logits(**{**good, name: P + 2}, check=False) == pkg.SHARD_EINVAL and "aligned" in pkg.shard_last_error()
+
+
 def test_work_refuses():
     for bad in ((0, 8, 2, 64), (4, 0, 2, 64), (4, 8, 0, 64), (4, 8, 3, 64), (4, 8, 2, 63)):
         with pytest.raises(pkg.ShardError) as e:
