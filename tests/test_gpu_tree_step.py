@@ -11,6 +11,7 @@ import numpy as np
 import pytest
 import torch
 
+import oracle
 import paper_2608_19147_gb300 as pkg
 import synth
 from gpu_engine import GpuEngine, GpuShard, to_dev
@@ -327,3 +328,67 @@ def test_a_request_without_a_token_is_an_error_and_changes_nothing(model):
         finally:
             d.close()
     assert outs[0] == outs[1]
+
+
+def test_sampled_trees_emit_the_models_draws(model):
+    """Sixteen requests of one text with trees of likely drafts: every emitted token is the draw of the model's distribution (the oracle's)
+    after the path before it, with the random number that its node was given, and a path goes on as long as the tree has the draw.
+    Logits differ from the oracle's by e at most: the head's bar (2e-3 and 1e-4 of the largest) and, for the step's 1e-3 of the hidden
+    state, four times that of the logits' spread; at temperature T a sum of weights then differs by exp(2 e / T) - 1 of the whole."""
+    stages, head = model
+    w, hw = synth.make_weights(synth.TINY, SEED), synth.make_head(synth.TINY.hidden, synth.TINY.vocab, synth.TINY.group, SEED + 1)
+    T, B, known, g = 0.1, 16, {}, np.random.default_rng(17)
+
+    def after(tokens):
+        """(weights that sum to 1, their sums by id, how far a sum may be off) after these tokens"""
+        key = tuple(tokens)
+        if key not in known:
+            n = len(key)
+            h = OracleEngine(synth.TINY, w, 1, 32).step([n], np.arange(n, dtype=np.int32), np.ones(n, np.uint8), token_ids=np.array(key, np.int32))
+            lg = oracle.head_top1(h[-1:], hw.norm, hw.lm_head, hw.rms_eps)[3][0]
+            x = np.exp((lg - lg.max()) / T)
+            e = 2e-3 + 1e-4 * np.abs(lg).max() + 4e-3 * lg.std()
+            known[key] = x / x.sum(), np.cumsum(x) / x.sum(), np.exp(2 * e / T) - 1
+        return known[key]
+
+    def is_draw(token, u, tokens):
+        p, upto, off = after(tokens)
+        return upto[token] - p[token] - off <= u <= upto[token] + off
+
+    given = [np.full(B, 0.4)]
+    d = TreeDecoder(stages, synth.TINY.hidden, head, B, 80, temperature=T, draws=lambda n: given[-1][:n])
+    try:
+        text = PROMPTS[0]
+        first = d.prefill([text] * B)
+        assert len(set(first)) == 1 and is_draw(first[0], 0.4, text)
+        text = text + first[:1]
+        p, upto, _ = after(text)
+        kids = [int(t) for t in np.argsort(-p)[:3]]
+        drafts, parents = list(kids), [0] * 3
+        for k, t in enumerate(kids):
+            for c in np.argsort(-after(text + [t])[0])[:3]:
+                drafts.append(int(c))
+                parents.append(1 + k)
+        n = 1 + len(drafts)
+        u = g.random((B, n))
+        for b in range(3):  # the middle of a draft's share, further from its ends than sums are off: surely that draft
+            u[b, 0] = upto[kids[b]] - p[kids[b]] / 2
+        given.append(u.reshape(-1))
+        out = d.step([(drafts, parents)] * B)
+        lengths = set()
+        for b in range(B):
+            node, path = 0, []
+            for k, token in enumerate(out[b]):
+                assert is_draw(token, np.float32(u[b, node]), text + path), (b, k)
+                path.append(token)
+                node = next((1 + i for i in range(len(drafts)) if parents[i] == node and drafts[i] == token), None)
+                assert (node is None) == (k + 1 == len(out[b])), (b, k)
+            lengths.add(len(out[b]))
+        for b in range(3):
+            assert p[kids[b]] / 2 <= after(text)[2] or out[b][0] == kids[b]
+        assert len(lengths) > 1 and any(p[t] / 2 > after(text)[2] for t in kids)
+        given.append(g.random(B))
+        for b, token in enumerate(d.step()):
+            assert is_draw(token[0], np.float32(given[-1][b]), text + out[b]), b
+    finally:
+        d.close()
