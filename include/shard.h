@@ -395,8 +395,8 @@ int shard_step_tree(shard_t shard, kvstate_t state, const uint16_t* hidden_in, c
  *            lens[b] + i of row b become 1 for kept nodes and 0 for the rest
  *            (the mask-based rewind); both NULL for none
  * path_stride is at least the largest tree's nodes; a request for which it is
- * not, or whose tree_start or lens is out of range, is left out.  A node whose
- * parent is out of range is not kept.  Runs on the device that holds parents;
+ * not, or whose tree_start or lens is out of range, is left out.  A node behind
+ * node 0 whose parent is out of range is not kept (node 0 is).  Runs on the device that holds parents;
  * asynchronous on cuda_stream.  Errors: EINVAL, ECUDA. */
 int shard_tree_accept(int B, int N, const int32_t* tree_start, const int32_t* parents, const int32_t* drafts,
                       const int32_t* targets, int path_stride, int32_t* path, int32_t* tokens, int32_t* count,

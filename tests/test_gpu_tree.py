@@ -625,6 +625,13 @@ def test_accept_leaves_out_what_is_wrong():
     assert status == pkg.SHARD_TREE_START and count.tolist() == [3, 0, 0]
 
 
+def test_accept_keeps_node_0_whatever_its_parent():
+    start, zero = np.array([0, 3], np.int32), np.zeros(3, np.int32)
+    for first in (-1, 0, 2, -7):
+        path, _, count, _, status = run_accept(start, np.array([first, 0, 1], np.int32), zero, zero, 3, None, None)
+        assert path.tolist() == [[0, 1, 2]] and count.tolist() == [3] and status == (0 if first == -1 else pkg.SHARD_TREE_PARENT)
+
+
 def test_accept_refusals():
     x = torch.zeros(16, dtype=torch.int32, device="cuda").data_ptr()
     def rc(*a, **k):
