@@ -22,6 +22,8 @@
 // min_p 0.02 118 (0.55 TB/s), 16 rows without filters 24, with top_p 0.9 alone 80.  A row's
 // chain of barriers and passes bounds it, not memory: a cluster barrier is 900 cycles, the
 // first histogram of a CTA's 8192 tokens 2500 (its atomics), a pass over exact weights 14000.
+// 64 registers, so that two CTAs fit an SM, spill 128 to 152 bytes a thread, also in the
+// launches that have one CTA to an SM.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 

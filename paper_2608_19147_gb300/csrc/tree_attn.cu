@@ -1173,10 +1173,11 @@ cudaError_t launch(Params& p, int device, int grid, long long units, cudaStream_
   using L = Geo<D, kF32, kBf16, kRows>;
   const int tiles = kF32 && p.a.out_type == SHARD_F32 ? L::kFold32 : L::kFold;
   p.fold = 2 * tiles;
-  // A stream's tiles in a piece are no more than the cache's and than a CTA's.  Where they are within p.fold, the kernel
-  // without the code for more (without / with: one stream, two caches of 95000 entries, 257 / 278 us; trees of 64 on 60000
-  // entries 214 to 225 / 222 to 226).
-  const bool take = std::min<long long>((p.a.capacity + kTile - 1) / kTile, (units + grid - 1) / grid) > tiles;
+  // A piece's tiles are no more than the cache's and than a CTA's, and two streams share those of 128 rows.  Where a
+  // stream's are within p.fold, the kernel without the code for more (without / with: two caches of 95000 entries 131 / 135
+  // us, one stream 257 / 278; trees of 64 on 60000 entries 214 to 225 / 222 to 226).
+  const long long piece = std::min<long long>((p.a.capacity + kTile - 1) / kTile, (units + grid - 1) / grid);
+  const bool take = (kRows == kTile && !L::kSingle ? (piece + 1) / 2 : piece) > tiles;
   cudaError_t e = take ? launch_kernel<D, kF32, kBf16, kRows, true>(p, device, grid, s) : launch_kernel<D, kF32, kBf16, kRows, false>(p, device, grid, s);
   if (e != cudaSuccess || grid < 2) return e;
   const long long rows = ((long long)p.a.N * p.a.n_kv_heads) << p.g_shift;

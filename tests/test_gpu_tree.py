@@ -547,6 +547,40 @@ def test_captured_graph_follows_the_lengths():
         c.check()
 
 
+@pytest.mark.parametrize("kv", ["f16", "bf16"])
+def test_captured_graphs_of_32_bit_queries_on_two_streams(kv):
+    """Sums taken over in `work`: graphs with a buffer each, replayed together with other lengths, as the eager calls."""
+    s, made = torch.cuda.Stream(), []
+    for seed in (1, 2):
+        c = Case([5, 40], [100, 500], 8, 2, 128, q="f32", kv=kv, cap=9000, mask=False, seed=seed)
+        c.k_at.normal_(), c.v_at.normal_()
+        c.run()  # loads the kernels
+        torch.cuda.synchronize()
+        work = torch.empty(pkg.shard_tree_attention_work(c.N, 8, 2, 128), dtype=torch.uint8, device="cuda")
+        start, parents, lens, _, _ = c.keep
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            pkg.shard_tree_attention(c.q.data_ptr(), pkg.SHARD_F32, c.k_at.data_ptr(), c.v_at.data_ptr(), TYPES[kv][1], c.out.data_ptr(),
+                                     pkg.SHARD_F32, 2, c.N, 8, 2, 128, c.cap, c.strides, start.data_ptr(), parents.data_ptr(), lens.data_ptr(), None, 0,
+                                     work.data_ptr(), work.numel(), status=c.status.data_ptr(), stream=torch.cuda.current_stream().cuda_stream)
+        made.append((c, graph, lens, (start, parents, work)))
+    for more in ([8900, 3], [0, 8950], [4000, 5000]):
+        for c, _, lens, _ in made:
+            c.lens = more
+            lens.copy_(torch.tensor(more, dtype=torch.int32))
+        torch.cuda.synchronize()
+        for _ in range(3):
+            made[0][1].replay()
+            with torch.cuda.stream(s):
+                made[1][1].replay()
+        torch.cuda.synchronize()
+        for c, _, _, _ in made:
+            assert c.status.item() == 0 and relative(c, exact(c)) <= 2.0 ** -19
+            first = c.out.clone()
+            c.run()
+            assert torch.equal(first, c.out)
+
+
 def test_two_streams_with_a_work_buffer_each():
     a, b = Case([9, 2], [3000, 100], 8, 2, 64, seed=1), Case([1, 30], [50, 4000], 8, 2, 64, seed=2)
     s, t = torch.cuda.Stream(), torch.cuda.Stream()
