@@ -40,9 +40,9 @@
 // fp16 on 95000 entries, 48 instead of 40 for 16 requests).
 //
 // Measured (GB300, calls replayed): one node on 100 entries 9.2 us, 16 requests of
-// 5 nodes on 128 to 2048 entries 28.5 (65 MB), 4 trees of 64 at 64 / 8 heads on 4096
-// entries 54.6 (34.6 GFLOP), the same two on 60000 entries 219 (1150 TFLOP/s), 2 of
-// 32 at 32 / 8 heads on 95000 entries 129 (5.9 TB/s).  Long caches are bound by
+// 5 nodes on 128 to 2048 entries 28.8 (65 MB), 4 trees of 64 at 64 / 8 heads on 4096
+// entries 54.7 (34.6 GFLOP), the same two on 60000 entries 225 (1120 TFLOP/s), 2 of
+// 32 at 32 / 8 heads on 95000 entries 131 (5.8 TB/s).  Long caches are bound by
 // memory; many rows by the chain S, softmax, P V of a stream's steps (the tensor
 // unit is 40 to 60 % busy); the rest by the kernels' starts, pieces' output and join.
 #include <algorithm>
