@@ -222,11 +222,18 @@ class TreeDecoder:
     def _dev(self, values, dtype):
         return self.torch.from_numpy(np.ascontiguousarray(values, dtype=dtype)).to("cuda")
 
-    def _sample(self, h, n: int):
-        """A draw from the model's distribution after each of n hidden rows (device int32 [n])."""
-        torch, stream = self.torch, self.torch.cuda.current_stream().cuda_stream
+    def _numbers(self, n: int) -> np.ndarray:
+        """n random numbers, before anything runs on them."""
+        u = np.asarray(self.draws(n), np.float32)
+        if u.shape != (n,):
+            raise ValueError("draws(%d) gave numbers of shape %r" % (n, u.shape))
+        return np.minimum(u, np.float32(1 - 2.0 ** -24))
+
+    def _sample(self, h, numbers: np.ndarray):
+        """A draw from the model's distribution after each hidden row, one per number (device int32 [n])."""
+        torch, stream, n = self.torch, self.torch.cuda.current_stream().cuda_stream, numbers.size
         token = torch.empty(n, dtype=torch.int32, device="cuda")
-        u = self._dev(np.minimum(np.asarray(self.draws(n), np.float32), np.float32(1 - 2.0 ** -24)), np.float32)
+        u = self._dev(numbers, np.float32)
         for i in range(0, n, SHARD_MAX_TOKENS):
             head_sample(self.head, h[i:].data_ptr(), min(SHARD_MAX_TOKENS, n - i), u[i:].data_ptr(), token[i:].data_ptr(),
                         **{k: v.data_ptr() for k, v in self.settings.items()}, stream=stream)
@@ -252,6 +259,7 @@ class TreeDecoder:
         for b, prompt in enumerate(prompts):
             if self.length[b] + len(prompt) > self.capacity:
                 raise ValueError("request %d would hold %d entries > %d" % (b, self.length[b] + len(prompt), self.capacity))
+        numbers = self._numbers(self.B)
         torch, stream = self.torch, self.torch.cuda.current_stream().cuda_stream
         last = torch.empty((self.B, self.hidden), dtype=torch.int16, device="cuda")
         for b, prompt in enumerate(prompts):
@@ -265,7 +273,7 @@ class TreeDecoder:
                               self.mask[b].data_ptr(), self.capacity, out.data_ptr(), stream)
                 h = out
             last[b] = h[n - 1]
-        token = self._sample(last, self.B)
+        token = self._sample(last, numbers)
         for sh in self.stages:
             shard_sync_status(sh, stream)
         first = token.tolist()
@@ -294,6 +302,7 @@ class TreeDecoder:
         torch, stream, N = self.torch, self.torch.cuda.current_stream().cuda_stream, sum(n)
         if N > SHARD_MAX_TREE_NODES:
             raise ValueError("%d nodes in all > %d" % (N, SHARD_MAX_TREE_NODES))
+        numbers = self._numbers(N)
         start = self._dev(np.concatenate([[0], np.cumsum(n)]), np.int32)
         ids, up = self._dev(sum(tokens, []), np.int32), self._dev(sum(parents, []), np.int32)
         pos = self._dev([self.position[b] + d for b in range(self.B) for d in depths[b]], np.int32)
@@ -306,7 +315,7 @@ class TreeDecoder:
             shard_step_tree(sh, st, None if h is None else h.data_ptr(), ids.data_ptr() if h is None else None, n, up.data_ptr(),
                             pos.data_ptr(), self.mask.data_ptr(), self.capacity, out.data_ptr(), stream)
             h = out
-        target = self._sample(h, N)
+        target = self._sample(h, numbers)
         path, emitted = (torch.empty((self.B, max(n)), dtype=torch.int32, device="cuda") for _ in range(2))
         count = torch.empty(self.B, dtype=torch.int32, device="cuda")
         shard_tree_accept(self.B, N, start.data_ptr(), up.data_ptr(), ids.data_ptr(), target.data_ptr(), max(n), path.data_ptr(),

@@ -330,6 +330,24 @@ def test_a_request_without_a_token_is_an_error_and_changes_nothing(model):
     assert outs[0] == outs[1]
 
 
+def test_draws_of_another_count_are_refused_before_anything_runs(model):
+    stages, head = model
+    d = TreeDecoder(stages, synth.TINY.hidden, head, 2, 40, draws=lambda n: np.full(n, 0.3))
+    good = d.draws
+    try:
+        for f in (lambda: d.prefill([[1, 2], [3]]), lambda: d.step([([5], [0]), ((), ())])):
+            for bad in (lambda n: np.zeros(n - 1), lambda n: np.zeros(n + 1), lambda n: np.zeros((1, n)), lambda n: 0.5):
+                d.draws, before = bad, (list(d.length), list(d.current))
+                with pytest.raises(ValueError, match="draws"):
+                    f()
+                assert (d.length, d.current) == before
+                assert [[pkg.kv_state_length(st, b) for b in range(2)] for st in d.states] == [d.length] * 2
+            d.draws = good
+            f()
+    finally:
+        d.close()
+
+
 def test_sampled_trees_emit_the_models_draws(model):
     """Sixteen requests of one text with trees of likely drafts: every emitted token is the draw of the model's distribution (the oracle's)
     after the path before it, with the random number that its node was given, and a path goes on as long as the tree has the draw.
