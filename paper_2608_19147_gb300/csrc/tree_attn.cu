@@ -67,14 +67,6 @@ constexpr int kSoft = 256;      // softmax threads
 // when it has been passed by 2^8: a weight is below 2^14, within fp16, and fp16
 // still holds weights 2^-20 of the largest with all its bits.
 constexpr float kLift = 6.f, kLag = 8.f;
-// The tensor unit cuts the bits that a sum of 32 bits has no room for off, always toward zero: O loses some 2^-25 of
-// itself with each product added, 3e-5 over 64 tiles of three parts.  So O is taken over into a sum of its own, rounded to
-// nearest, after so many of a stream's tiles: one or two where both queries and outputs have 32 bits (error 5.4e-7 to 7e-7 of
-// the result on one to 256 tiles per CTA, 8.2e-7 with two, where it was 2.7e-5 after 64 and 1e-4 after 256), else where the
-// loss would come near the weights' rounding.  The sum is in tensor memory where that has room (head_dim 64; one stream,
-// whose sums the idle warps of the other take), else in `work`.  Times of two caches of 95000 entries, 32-bit queries and
-// outputs, without and with it: fp16 179 / 225 us (every tile 256), bf16 257 / 283; head_dim 64, fp16, 114 / 135; 5 nodes
-// instead of 32, fp16, 158 / 174.
 constexpr float kMost = 3.402823466e38f;  // the largest finite value
 
 struct Params {
@@ -103,7 +95,14 @@ struct Geo {
   static constexpr int kParts = !kF32 ? 1 : kBf16 ? 3 : 2;  // of 11 or 8 bits of a 32-bit value
   static constexpr bool kSingle = kParts == 3;              // one stream: the other's S is where the third parts of P go
   static constexpr bool kSpare = kSingle || D == 64;        // tensor memory has room for the sums that O is taken over into
-  // tiles of a stream from one to the next: 32-bit queries and outputs; else some 1000 products or 1500 (3e-5 to 5e-5)
+  // The tensor unit cuts off the bits that a sum of 32 bits has no room for, always toward zero: O loses some 2^-25 of itself
+  // with each product added, 3e-5 over 64 tiles of three parts.  So a stream takes its O over into a sum of its own, rounded
+  // to nearest, after kFold32 tiles with 32-bit queries and outputs (error 5.4e-7 to 7e-7 of the result on one to 256 tiles
+  // per CTA, 8.2e-7 by two tiles, where it was 2.7e-5 after 64 and 1e-4 after 256), else after kFold (some 1000 products or
+  // 1500: 3e-5 to 5e-5, which the weights' or the outputs' rounding covers).  The sum is in tensor memory where that has
+  // room (head_dim 64; one stream, whose sums the idle warps of the other take), else in `work`.  Two caches of 95000
+  // entries, 32-bit queries and outputs, without and with it: fp16 179 / 225 us (every tile 256), bf16 257 / 283; head_dim 64,
+  // fp16, 114 / 135; 5 nodes instead of 32, fp16, 158 / 174.
   static constexpr int kFold32 = kSpare ? 1 : 2, kFold = kParts == 1 ? 128 : 64;
   static constexpr int kQTiles = kF32 ? kParts : kRows / kTile;
   static constexpr uint32_t kBlock = kTile * 128;        // 64 columns of a tile of K, V or Q
